@@ -61,11 +61,21 @@ extern "C" {
 #define TSLT_F32 0
 #define TSLT_BF16 1
 
+#define TSLT_STATUS_WAIT_TIMEOUT 4   /* a bounded wait inside a product kernel ran out; outputs of that call are invalid */
+#define TSLT_STATUS_BAD_TARGET 8     /* a target token was >= V; that row was taken as ignored */
+
 /* largest supported k (top-k size, or the candidate cap when top-p is on) */
 #define TSLT_MAX_K 1024
 
 /* most vocabulary shards one tslt_sparsify_merge takes; it also needs nshards * k <= 2048 */
 #define TSLT_MAX_SHARDS 16
+
+/* limits of the output head's calls: hidden size; hidden size of the 8-bit head product (its sums stay
+ * inside 32 bits: 128 * 128 * 65536 = 2^30); rows and vocabulary of the loss */
+#define TSLT_MAX_HIDDEN 16384
+#define TSLT_MAX_INT8_K 65536
+#define TSLT_MAX_LOSS_ROWS (1 << 20)
+#define TSLT_MAX_LOSS_VOCAB (1 << 24)
 
 /* size of the scratch array built into the library for tslt_verify_static */
 #define TSLT_STATIC_SCRATCH_BYTES (8u << 20)
@@ -351,6 +361,69 @@ int tslt_diagnostics(const void* draft_logits, const void* target_logits, int dt
                      float draft_temperature, float target_temperature, float* beta_j, float* z_j,
                      float* theta, float* rho, float* beta_hat_j, float* theta_hat, void* workspace,
                      size_t workspace_bytes, void* stream);
+
+/*
+ * The output head around the logits (not from the paper, which starts at the models' distributions): what
+ * a draft or target model runs between its last layer and tslt_sparsify / tslt_verify, and what trains the
+ * draft's head.
+ *
+ * tslt_rmsnorm_quant: residual addition, RMS norm and quantisation of the hidden states, one pass.  For each row
+ *   h = x + residual (rounded to the storage type; h = x without a residual);
+ *   v = h * weight (fp32; weight may be NULL: 1), y = v / sqrt(mean(h^2) + eps);
+ *   scale = max|y| / 127, q = rint(127 v / max|v|) in [-127, 127], ties to even, so that y ~ q * scale.
+ * A row of zeros gives q = 0, scale = 0; a row with a NaN or an infinity gives a scale that is NaN.  (Sums of squares are
+ * held in fp32: elements above about 1e17 overflow them, and the scale of such a row is 0.)
+ * x, residual, weight and residual_out are TSLT_F32 or TSLT_BF16, all the same; residual and residual_out (which gets h) are
+ * nullable; residual_out may be x or residual itself (same pointer and stride), no other overlap is allowed.
+ * tslt_quantize_rows: the same quantiser without norm and weight (y = x): lays a head weight [V, D] out once for
+ * tslt_head_logits, one scale per vocabulary entry.
+ * Rows: x [rows, D] with a stride; q [rows, D] int8 with a stride; scale [rows] fp32.  Every base pointer 16-byte aligned,
+ * every stride a multiple of 16 bytes; D itself may be any number from 1 to TSLT_MAX_HIDDEN.  No workspace.
+ */
+int tslt_rmsnorm_quant(const void* x, const void* residual, const void* weight, int dtype, int rows, int D,
+                       long long x_stride, long long residual_stride, float eps, void* residual_out,
+                       long long out_stride, signed char* q, long long q_stride, float* scale, void* stream);
+int tslt_quantize_rows(const void* x, int dtype, int rows, int D, long long x_stride, signed char* q,
+                       long long q_stride, float* scale, void* stream);
+
+/*
+ * The head product in 8-bit integers: logits[n, v] = q_scale[n] * weight_scale[v] * sum_k q[n, k] weight[v, k].  The sum is
+ * exact (32-bit integers on the tensor cores); the scales are applied in fp32 (sum, times q_scale, times
+ * weight_scale) and the result is rounded once to logits_dtype (TSLT_F32 or TSLT_BF16).  The logits are laid out as
+ * tslt_sparsify, tslt_verify and tslt_tree_verify read them.
+ * q [rows, D] and weight [V, D] int8 (-128 is allowed), logits [rows, V], each with a row stride (elements); base pointers
+ * 16-byte aligned, strides multiples of 16 bytes; rows, V and D may be any numbers, D <= TSLT_MAX_INT8_K.  Elements between
+ * V and logits_stride are left as they are.  Workspace >= 256 bytes (the status word), 256-byte aligned.
+ */
+int tslt_head_logits(const signed char* q, const float* q_scale, long long q_stride, const signed char* weight,
+                     const float* weight_scale, long long weight_stride, int rows, int V, int D, int logits_dtype,
+                     void* logits, long long logits_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Softmax cross entropy of a linear head, z = hidden weight^T (bf16 operands, fp32 sums), computed in pieces of
+ * the vocabulary without keeping the logits:
+ *   lse[n] = ln sum_v exp z[n, v],  loss[n] = lse[n] - z[n, target[n]].
+ * A row with target < 0 is ignored: loss = lse = 0 there, and its hidden row is never used (it may hold anything,
+ * NaN included).  target >= V is taken as ignored too and sets TSLT_STATUS_BAD_TARGET.
+ * tslt_linear_ce_backward: with dloss[n] the derivative of the caller's total by loss[n] (NULL: 1 everywhere) and
+ * G[n, v] = dloss[n] (exp(z[n, v] - lse[n]) - [v = target[n]]) (0 in ignored rows),
+ *   dhidden = G weight,  dweight = G^T hidden,
+ * both overwritten whole (zeros for ignored rows; zeros in dweight when no row counts).  lse is what tslt_linear_ce
+ * wrote.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
+ * own rounding); sums are fp32 and their order is fixed: the same inputs give the same bits.
+ * hidden, dhidden [rows, D], weight, dweight [V, D]: bf16 with row strides (elements, multiples of 8), 16-byte aligned;
+ * target [rows] int32; loss, lse, dloss [rows] fp32.  rows = 0 is allowed (dweight = 0).  D <= TSLT_MAX_HIDDEN, rows <=
+ * TSLT_MAX_LOSS_ROWS, V <= TSLT_MAX_LOSS_VOCAB.  Outputs must not overlap inputs.
+ */
+int tslt_linear_ce_workspace_bytes(int rows, int V, int D, size_t* bytes);
+int tslt_linear_ce(const void* hidden, long long hidden_stride, const void* weight, long long weight_stride,
+                   const int* target, int rows, int V, int D, float* loss, float* lse, void* workspace,
+                   size_t workspace_bytes, void* stream);
+int tslt_linear_ce_backward_workspace_bytes(int rows, int V, int D, size_t* bytes);
+int tslt_linear_ce_backward(const void* hidden, long long hidden_stride, const void* weight, long long weight_stride,
+                            const int* target, const float* lse, const float* dloss, int rows, int V, int D,
+                            void* dhidden, long long dhidden_stride, void* dweight, long long dweight_stride,
+                            void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,245 @@
+// RMS norm with the residual's addition and an 8-bit output (tslt_rmsnorm_quant), and the same quantiser
+// without the norm (tslt_quantize_rows).
+//
+// Mathematics.  h = x + r in the storage type; v = h w; the normalised row is y = v / rms(h), and its codes are
+// q = rint(127 y / max|y|) with scale = max|y| / 127.  The row's 1 / rms cancels out of q: q = rint(127 v / max|v|).
+// So the sum of squares and the maximum are needed from ONE pass over the row and one block reduction gives both;
+// the row stays in registers between them and is read and written once.  Bound by HBM: 2 + 2 + 2 + 1 bytes an
+// element (bf16 with a residual).
+//
+// Rounding.  t = v * (127 / max|v|) in fp32 is off by at most 1.5 * 2^-23 * 127 = 2.3e-5; where t lies within 1e-4 of
+// the border between two codes (one element in 5000), the code is taken from the quotient in fp64 instead, so that
+// every code is the nearest one to the exact quotient of the fp32 values v and max|v|.  (For bf16 h and w the product
+// v is exact.)
+#include "tslt_common.cuh"
+
+namespace tslt {
+
+struct NormParams {
+    const void *x, *r, *w;  // r, w may be null
+    void* h;                // may be null; may equal x or r
+    int8_t* q;
+    float* scale;
+    long long xs, rs, hs, qs;  // row strides in elements
+    int rows, D;
+    float eps;
+};
+
+__device__ __forceinline__ int code_of(float v, float top, float inv) {
+    const float t = v * inv;
+    float c = rintf(t);
+    // A NaN t (v or top not finite, or top so small that inv overflowed) fails the comparison too.
+    if (!(fabsf(t - c) < 0.4999f)) {
+        const double e = rint(127.0 * (double)v / (double)top);
+        c = e == e ? fminf(fmaxf((float)e, -127.f), 127.f) : 0.f;
+    }
+    return (int)c;
+}
+
+// fp32 -> storage type, round to nearest even (bf16 patterns built by hand would cost more than the conversion)
+template <typename T> __device__ __forceinline__ void add_round(float* a, const float* b);
+template <> __device__ __forceinline__ void add_round<float>(float* a, const float* b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __fadd_rn(a[i], b[i]);
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {  // lo in the low half
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+template <> __device__ __forceinline__ void add_round<bf16_t>(float* a, const float* b) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const uint32_t d = pack_bf16x2(__fadd_rn(a[i], b[i]), __fadd_rn(a[i + 1], b[i + 1]));
+        a[i] = __uint_as_float(d << 16);
+        a[i + 1] = __uint_as_float(d & 0xffff0000u);
+    }
+}
+
+// The vector of elements [at, at + kPerVec) of a row of D; past the row's end (its last vector may be short) zeros.
+template <typename T> __device__ __forceinline__ uint4 load_elems(const void* row, int at, int D) {
+    constexpr int P = Elt<T>::kPerVec;
+    const char* p = (const char*)row + (size_t)at * Elt<T>::kBytes;
+    if (at + P <= D) return *reinterpret_cast<const uint4*>(p);
+    float z[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) z[i] = at + i < D ? Elt<T>::load(row, at + i) : 0.f;
+    return pack_vec<T>(z);
+}
+template <typename T> __device__ __forceinline__ void store_elems(void* row, int at, int D, const float* z) {
+    constexpr int P = Elt<T>::kPerVec;
+    const uint4 v = pack_vec<T>(z);
+    char* p = (char*)row + (size_t)at * Elt<T>::kBytes;
+    if (at + P <= D) {
+        *reinterpret_cast<uint4*>(p) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            if (at + i < D) {
+                if (Elt<T>::kBytes == 4) reinterpret_cast<float*>(p)[i] = z[i];
+                else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(__float_as_uint(z[i]) >> 16);
+            }
+        }
+    }
+}
+
+// One CTA per row; thread t holds vectors t, t + nthreads, ... (NV of them).
+template <typename T, int NV, bool kNorm>
+__global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024) norm_quant_kernel(const __grid_constant__ NormParams p) {
+    constexpr int P = Elt<T>::kPerVec;
+    __shared__ float s_sum[32], s_top[32];
+    const int tid = threadIdx.x, nth = blockDim.x, nwarps = nth >> 5;
+    const long long row = blockIdx.x;
+    const char* x = (const char*)p.x + row * p.xs * Elt<T>::kBytes;
+    const char* r = p.r ? (const char*)p.r + row * p.rs * Elt<T>::kBytes : nullptr;
+    uint4 xv[NV], rv[NV], wv[NV];  // every load of the row is in flight before the first is used
+#pragma unroll
+    for (int j = 0; j < NV; ++j) xv[j] = load_elems<T>(x, (tid + j * nth) * P, p.D);
+    if (kNorm && r) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) rv[j] = load_elems<T>(r, (tid + j * nth) * P, p.D);
+    }
+    if (kNorm && p.w) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) wv[j] = load_elems<T>(p.w, (tid + j * nth) * P, p.D);
+    }
+    float v[NV][P];
+    float sum = 0.f, top = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) unpack_vec<T>(xv[j], v[j]);
+    if (kNorm && r) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float b[P];
+            unpack_vec<T>(rv[j], b);
+            add_round<T>(v[j], b);
+        }
+    }
+    if (kNorm && p.h) {
+        char* h = (char*)p.h + row * p.hs * Elt<T>::kBytes;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int at = (tid + j * nth) * P;
+            if (at < p.D) store_elems<T>(h, at, p.D, v[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (kNorm) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum = fmaf(v[j][i], v[j][i], sum);
+            if (p.w) {
+                float w[P];
+                unpack_vec<T>(wv[j], w);
+#pragma unroll
+                for (int i = 0; i < P; ++i) v[j][i] = __fmul_rn(v[j][i], w[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum += v[j][i] * 0.f;  // carries a NaN or infinity into the scale
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i) top = fmaxf(top, fabsf(v[j][i]));
+    }
+    sum = warp_sum(sum);
+    top = warp_max(top);
+    if ((tid & 31) == 0) {
+        s_sum[tid >> 5] = sum;
+        s_top[tid >> 5] = top;
+    }
+    __syncthreads();
+    sum = 0.f;
+    top = 0.f;
+    for (int w = 0; w < nwarps; ++w) {  // the same order in every thread
+        sum += s_sum[w];
+        top = fmaxf(top, s_top[w]);
+    }
+    if (tid == 0) {
+        float s;
+        if (kNorm) {
+            const float rstd = (float)(1.0 / sqrt((double)sum / p.D + (double)p.eps));
+            s = top * rstd / 127.f;
+            if (top == 0.f && sum == sum) s = 0.f;
+        } else {
+            s = top / 127.f + sum;
+        }
+        p.scale[row] = s;
+    }
+    const float inv = top > 0.f ? 127.f / top : 0.f;
+    int8_t* q = p.q + row * p.qs;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int at = (tid + j * nth) * P;
+        if (at >= p.D) break;
+        uint32_t c[P / 4];
+#pragma unroll
+        for (int i = 0; i < P / 4; ++i) {
+            c[i] = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c[i] |= ((uint32_t)code_of(v[j][4 * i + k], top, inv) & 0xffu) << (8 * k);
+        }
+        if (at + P <= p.D) {
+            if (P == 8) *reinterpret_cast<uint2*>(q + at) = make_uint2(c[0], c[P / 4 - 1]);
+            else *reinterpret_cast<uint32_t*>(q + at) = c[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (at + i < p.D) q[at + i] = (int8_t)(c[i / 4] >> (8 * (i % 4)));
+        }
+    }
+}
+
+constexpr int kMaxHidden = TSLT_MAX_HIDDEN;
+
+template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cudaStream_t st) {
+    const int nvec = (p.D + Elt<T>::kPerVec - 1) / Elt<T>::kPerVec;
+    // Few rows: latency counts, so a row is spread over as many threads as it has vectors.  Rows enough to fill the
+    // machine: several vectors in flight per thread.
+    int nv = p.rows < 2 * 148 ? 1 : (nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1);
+    while ((nvec + nv - 1) / nv > 1024) nv *= 2;
+    const int threads = ((nvec + nv - 1) / nv + 31) / 32 * 32;
+    if (nv == 1) norm_quant_kernel<T, 1, kNorm><<<p.rows, threads, 0, st>>>(p);
+    else if (nv == 2) norm_quant_kernel<T, 2, kNorm><<<p.rows, threads, 0, st>>>(p);
+    else norm_quant_kernel<T, 4, kNorm><<<p.rows, threads, 0, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+}
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+static int elt_bytes(int dtype) { return dtype == TSLT_F32 ? 4 : 2; }
+static bool row_ok(const void* p, long long stride, int D, int bytes) {
+    return p && aligned16(p) && stride >= D && stride * bytes % 16 == 0;
+}
+
+}  // namespace tslt
+
+using namespace tslt;
+
+extern "C" int tslt_rmsnorm_quant(const void* x, const void* residual, const void* weight, int dtype, int rows, int D,
+                                  long long x_stride, long long residual_stride, float eps, void* residual_out,
+                                  long long out_stride, signed char* q, long long q_stride, float* scale, void* stream) {
+    if (dtype != TSLT_F32 && dtype != TSLT_BF16) return TSLT_ERR_UNSUPPORTED;
+    if (rows < 0 || D <= 0 || !(eps >= 0.f)) return TSLT_ERR_INVALID_ARG;
+    if (D > kMaxHidden) return TSLT_ERR_UNSUPPORTED;
+    if (rows == 0) return TSLT_OK;
+    const int b = elt_bytes(dtype);
+    if (!row_ok(x, x_stride, D, b) || !row_ok(q, q_stride, D, 1) || !scale) return TSLT_ERR_INVALID_ARG;
+    if (residual && !row_ok(residual, residual_stride, D, b)) return TSLT_ERR_INVALID_ARG;
+    if (residual_out && !row_ok(residual_out, out_stride, D, b)) return TSLT_ERR_INVALID_ARG;
+    if (weight && !aligned16(weight)) return TSLT_ERR_INVALID_ARG;
+    NormParams p = {x, residual, weight, residual_out, (int8_t*)q, scale, x_stride, residual_stride, out_stride, q_stride,
+                    rows, D, eps};
+    return dtype == TSLT_F32 ? launch_norm<float, true>(p, (cudaStream_t)stream)
+                             : launch_norm<bf16_t, true>(p, (cudaStream_t)stream);
+}
+
+extern "C" int tslt_quantize_rows(const void* x, int dtype, int rows, int D, long long x_stride, signed char* q,
+                                  long long q_stride, float* scale, void* stream) {
+    if (dtype != TSLT_F32 && dtype != TSLT_BF16) return TSLT_ERR_UNSUPPORTED;
+    if (rows < 0 || D <= 0) return TSLT_ERR_INVALID_ARG;
+    if (D > kMaxHidden) return TSLT_ERR_UNSUPPORTED;
+    if (rows == 0) return TSLT_OK;
+    if (!row_ok(x, x_stride, D, elt_bytes(dtype)) || !row_ok(q, q_stride, D, 1) || !scale) return TSLT_ERR_INVALID_ARG;
+    NormParams p = {x, nullptr, nullptr, nullptr, (int8_t*)q, scale, x_stride, 0, 0, q_stride, rows, D, 0.f};
+    return dtype == TSLT_F32 ? launch_norm<float, false>(p, (cudaStream_t)stream)
+                             : launch_norm<bf16_t, false>(p, (cudaStream_t)stream);
+}

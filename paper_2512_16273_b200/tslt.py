@@ -8,6 +8,7 @@ built library, or calling it with CPU tensors, raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional, Sequence
 
@@ -30,7 +31,10 @@ EXPORTS = ["tslt_version", "tslt_status_string", "tslt_workspace_status", "tslt_
            "tslt_tree_verify_walk_workspace_bytes", "tslt_tree_verify_walk",
            "tslt_payload_words", "tslt_pack_payload", "tslt_unpack_payload",
            "tslt_verify_packed", "tslt_tree_verify_packed",
-           "tslt_diagnostics_workspace_bytes", "tslt_diagnostics"]
+           "tslt_diagnostics_workspace_bytes", "tslt_diagnostics",
+           "tslt_rmsnorm_quant", "tslt_quantize_rows", "tslt_head_logits",
+           "tslt_linear_ce_workspace_bytes", "tslt_linear_ce",
+           "tslt_linear_ce_backward_workspace_bytes", "tslt_linear_ce_backward"]
 
 PROB_F32, PROB_BF16, PROB_F16 = 0, 1, 2
 
@@ -100,6 +104,20 @@ def lib() -> ctypes.CDLL:
     L.tslt_pack_payload.argtypes = [p, p, p, i, i, i, i, p, p, p]
     L.tslt_unpack_payload.restype = i
     L.tslt_unpack_payload.argtypes = [p, i, i, i, i, p, p, p, p, p]
+    L.tslt_rmsnorm_quant.restype = i
+    L.tslt_rmsnorm_quant.argtypes = [p, p, p, i, i, i, ll, ll, f, p, ll, p, ll, p, p]
+    L.tslt_quantize_rows.restype = i
+    L.tslt_quantize_rows.argtypes = [p, i, i, i, ll, p, ll, p, p]
+    L.tslt_head_logits.restype = i
+    L.tslt_head_logits.argtypes = [p, p, ll, p, p, ll, i, i, i, i, p, ll, p, sz, p]
+    L.tslt_linear_ce_workspace_bytes.restype = i
+    L.tslt_linear_ce_workspace_bytes.argtypes = [i, i, i, psz]
+    L.tslt_linear_ce.restype = i
+    L.tslt_linear_ce.argtypes = [p, ll, p, ll, p, i, i, i, p, p, p, sz, p]
+    L.tslt_linear_ce_backward_workspace_bytes.restype = i
+    L.tslt_linear_ce_backward_workspace_bytes.argtypes = [i, i, i, psz]
+    L.tslt_linear_ce_backward.restype = i
+    L.tslt_linear_ce_backward.argtypes = [p, ll, p, ll, p, p, p, i, i, i, p, ll, p, ll, p, sz, p]
     _lib = L
     return L
 
@@ -224,6 +242,8 @@ def workspace_status(ws: torch.Tensor) -> int:
 
 STATUS_WAIT_FELL_BACK = 1
 STATUS_BAD_RECORD = 2
+STATUS_WAIT_TIMEOUT = 4
+STATUS_BAD_TARGET = 8
 
 
 def set_ready_poll_limit(polls: int) -> None:
@@ -700,5 +720,273 @@ def diagnostics(draft_logits: torch.Tensor, target_logits: torch.Tensor, k_list:
                                 _ptr(o["beta_j"]), _ptr(o["z_j"]), _ptr(o["theta"]), _ptr(o["rho"]), _ptr(o["beta_hat_j"]),
                                 _ptr(o["theta_hat"]), _ptr(ws), ws.numel(), _stream())
     _check(rc, "tslt_diagnostics")
+    o["workspace"] = ws
+    return o
+
+
+# ---- the output head around the logits ---------------------------------------------------------------------
+MAX_HIDDEN = 16384
+MAX_INT8_K = 65536
+MAX_LOSS_ROWS = 1 << 20
+MAX_LOSS_VOCAB = 1 << 24
+
+
+def _own_device(call):
+    """Runs the call on its first argument's device (its current stream), whichever device is current."""
+    @functools.wraps(call)
+    def on_device(t, *args, **kw):
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != torch.cuda.current_device():
+            with torch.cuda.device(t.device):
+                return call(t, *args, **kw)
+        return call(t, *args, **kw)
+    return on_device
+
+
+def _matrix(t, name: str, dtype, dev: int, cols: Optional[int] = None):
+    """(rows, columns, row stride) of a CUDA tensor [..., columns] on device `dev` with evenly spaced rows."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor (libtslt has no CPU path)" % name)
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s must have dtype %s" % (name, dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is on another device" % name)
+    if t.dim() == 2:
+        rows, c = t.shape
+        stride = t.stride(0)
+        if c > 1 and t.stride(1) != 1:
+            raise ValueError("%s must be contiguous along its last dimension" % name)
+        if rows > 1 and stride < c:
+            raise ValueError("rows of %s overlap" % name)
+    elif t.dim() < 1:
+        raise ValueError("%s must have at least one dimension" % name)
+    else:
+        rows, c, stride = _row_layout(t)
+    if c < 1 or (cols is not None and c != cols):
+        raise ValueError("%s must have %s columns, has %d" % (name, "some" if cols is None else cols, c))
+    if rows <= 1:  # the stride of a single row says nothing
+        step = 16 // t.element_size()
+        stride = -(-c // step) * step
+    return rows, c, stride
+
+
+def _vector(t, name: str, dtype, dev: int, numel: int):
+    """A contiguous CUDA tensor of numel elements on device `dev`."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor (libtslt has no CPU path)" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s must have dtype %s" % (name, dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is on another device" % name)
+    if t.numel() != numel or not t.is_contiguous():
+        raise ValueError("%s must be contiguous with %d elements" % (name, numel))
+    return t
+
+
+def _rows_like(lead, cols: int, dtype, device) -> torch.Tensor:
+    """An empty [*lead, cols] whose rows start on 16-byte boundaries."""
+    step = 16 // (torch.finfo(dtype).bits // 8 if dtype.is_floating_point else 1)
+    wide = -(-cols // step) * step
+    t = torch.empty(*lead, wide, dtype=dtype, device=device)
+    return t if wide == cols else t[..., :cols]
+
+
+def _scratch(nbytes: int, device) -> torch.Tensor:
+    """The stream's cached workspace; under graph capture a buffer of the graph's own, so that two captured graphs
+    never share one."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(max(int(nbytes), 4096), dtype=torch.uint8, device=device)
+    return workspace(nbytes, device)
+
+
+def _space(ws, nbytes: int, device, dev: int) -> torch.Tensor:
+    if ws is None:
+        return _scratch(nbytes, device)
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_cuda or ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous uint8 CUDA tensor on the call's device")
+    return ws
+
+
+@_own_device
+def rmsnorm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                  eps: float = 1e-6, *, out: Optional[dict] = None) -> dict:
+    """tslt_rmsnorm_quant on hidden states x [..., D] (fp32 / bf16), weight [D] and residual [..., D] of the same type.
+
+    Returns dict(q [..., D] int8, scale [rows] fp32, and with a residual residual [..., D] = x + residual), q * scale
+    being the normalised rows.  `out` may hold any of them; out["residual"] may be x or residual itself."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor (libtslt has no CPU path)")
+    code, dev, device = _dtype_code(x), x.get_device(), x.device
+    rows, D, xs = _matrix(x, "x", None, dev)
+    rs = hs = 0
+    if residual is not None:
+        if residual.shape != x.shape:
+            raise ValueError("residual must have the shape of x")
+        rs = _matrix(residual, "residual", x.dtype, dev, D)[2]
+    if weight is not None:
+        _vector(weight, "weight", x.dtype, dev, D)
+    o = out if out is not None else {}
+    if "q" not in o:
+        o["q"] = _rows_like(x.shape[:-1], D, torch.int8, device)
+    if "scale" not in o:
+        o["scale"] = torch.empty(rows, dtype=torch.float32, device=device)
+    if residual is not None and "residual" not in o:
+        o["residual"] = _rows_like(x.shape[:-1], D, x.dtype, device)
+    h = o.get("residual")
+    if o["q"].shape != x.shape or (h is not None and h.shape != x.shape):
+        raise ValueError("outputs q and residual must have the shape of x")
+    qs = _matrix(o["q"], "q", torch.int8, dev, D)[2]
+    if h is not None:
+        hs = _matrix(h, "output residual", x.dtype, dev, D)[2]
+    _vector(o["scale"], "scale", torch.float32, dev, rows)
+    _check(lib().tslt_rmsnorm_quant(_ptr(x), _ptr(residual), _ptr(weight), code, rows, D, xs, rs, eps, _ptr(h), hs,
+                                    _ptr(o["q"]), qs, _ptr(o["scale"]), _stream()), "tslt_rmsnorm_quant")
+    return o
+
+
+@_own_device
+def quantize_rows(x: torch.Tensor, *, out: Optional[dict] = None) -> dict:
+    """tslt_quantize_rows on x [..., D] (fp32 / bf16), e.g. a head weight [V, D] for head_logits.  Returns dict(q [..., D]
+    int8, scale [rows] fp32), q * scale being the nearest the 8 bits come to x."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor (libtslt has no CPU path)")
+    code, dev, device = _dtype_code(x), x.get_device(), x.device
+    rows, D, xs = _matrix(x, "x", None, dev)
+    o = out if out is not None else {}
+    if "q" not in o:
+        o["q"] = _rows_like(x.shape[:-1], D, torch.int8, device)
+    if "scale" not in o:
+        o["scale"] = torch.empty(rows, dtype=torch.float32, device=device)
+    if o["q"].shape != x.shape:
+        raise ValueError("output q must have the shape of x")
+    qs = _matrix(o["q"], "q", torch.int8, dev, D)[2]
+    _vector(o["scale"], "scale", torch.float32, dev, rows)
+    _check(lib().tslt_quantize_rows(_ptr(x), code, rows, D, xs, _ptr(o["q"]), qs, _ptr(o["scale"]), _stream()),
+           "tslt_quantize_rows")
+    return o
+
+
+@_own_device
+def head_logits(q: torch.Tensor, scale: torch.Tensor, weight: torch.Tensor, weight_scale: torch.Tensor,
+                logits_dtype: torch.dtype = torch.bfloat16, *, out: Optional[dict] = None,
+                ws: Optional[torch.Tensor] = None) -> dict:
+    """tslt_head_logits: q [..., D] int8 and scale [rows] as rmsnorm_quant writes them, weight [V, D] int8 and weight_scale
+    [V] as quantize_rows writes them.  Returns dict(logits [..., V] fp32 / bf16, workspace); sparsify, verify and tree_verify
+    take the logits as they are."""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor (libtslt has no CPU path)")
+    dev, device = q.get_device(), q.device
+    rows, D, qs = _matrix(q, "q", torch.int8, dev)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise ValueError("weight must be [V, D]")
+    V, _, wstride = _matrix(weight, "weight", torch.int8, dev, D)
+    _vector(scale, "scale", torch.float32, dev, rows)
+    _vector(weight_scale, "weight_scale", torch.float32, dev, V)
+    if logits_dtype not in (torch.float32, torch.bfloat16):
+        raise TsltError(ERR_UNSUPPORTED, "dtype %s" % logits_dtype)
+    o = out if out is not None else {}
+    if "logits" not in o:
+        o["logits"] = _rows_like(q.shape[:-1], V, logits_dtype, device)
+    z = o["logits"]
+    zr, _, zs = _matrix(z, "logits", logits_dtype, dev, V)
+    if zr != rows:
+        raise ValueError("output logits must have %d rows" % rows)
+    ws = _space(ws, 256, device, dev)
+    _check(lib().tslt_head_logits(_ptr(q), _ptr(scale), qs, _ptr(weight), _ptr(weight_scale), wstride, rows, V, D,
+                                  F32 if logits_dtype == torch.float32 else BF16, _ptr(z), zs, _ptr(ws), ws.numel(), _stream()),
+           "tslt_head_logits")
+    o["workspace"] = ws
+    return o
+
+
+@_own_device
+def sparsify_hidden(x: torch.Tensor, norm_weight: Optional[torch.Tensor], head: torch.Tensor, head_scale: torch.Tensor, k: int,
+                    top_p: float = 1.0, temperature: float = 1.0, uniforms: Optional[torch.Tensor] = None, *,
+                    residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    logits_dtype: torch.dtype = torch.bfloat16) -> dict:
+    """The draft side from the last layer's hidden states on: rmsnorm_quant, head_logits and sparsify, one after the other
+    on the current stream.  x, residual [..., D]; head [V, D] int8 and head_scale [V] from quantize_rows; the rest as in
+    sparsify.  Returns what sparsify returns, and logits [..., V] and (with a residual) residual [..., D]."""
+    n = rmsnorm_quant(x, norm_weight, residual, eps)
+    z = head_logits(n["q"], n["scale"], head, head_scale, logits_dtype)["logits"]
+    o = sparsify(z, k, top_p, temperature, uniforms, ws=_scratch(sparsify_workspace_bytes(z.numel() // z.shape[-1], z.shape[-1], k,
+                 0 if uniforms is None else uniforms.numel() // max(1, z.numel() // z.shape[-1])), x.device))
+    o["logits"] = z
+    if residual is not None:
+        o["residual"] = n["residual"]
+    return o
+
+
+def _loss_workspace_bytes(name: str, rows: int, V: int, D: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(lib(), name)(rows, V, D, ctypes.byref(n)), name)
+    return int(n.value)
+
+
+def linear_ce_workspace_bytes(rows: int, V: int, D: int) -> int:
+    return _loss_workspace_bytes("tslt_linear_ce_workspace_bytes", rows, V, D)
+
+
+def linear_ce_backward_workspace_bytes(rows: int, V: int, D: int) -> int:
+    return _loss_workspace_bytes("tslt_linear_ce_backward_workspace_bytes", rows, V, D)
+
+
+def _loss_inputs(hidden, weight, target):
+    if not isinstance(hidden, torch.Tensor) or not hidden.is_cuda:
+        raise ValueError("hidden must be a CUDA tensor (libtslt has no CPU path)")
+    if hidden.dtype != torch.bfloat16:
+        raise TsltError(ERR_UNSUPPORTED, "dtype %s" % hidden.dtype)
+    dev = hidden.get_device()
+    rows, D, hs = _matrix(hidden, "hidden", None, dev)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise ValueError("weight must be [V, D]")
+    V, _, wstride = _matrix(weight, "weight", torch.bfloat16, dev, D)
+    _vector(target, "target", torch.int32, dev, rows)
+    return dev, rows, V, D, hs, wstride
+
+
+@_own_device
+def linear_ce(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, *, out: Optional[dict] = None,
+              ws: Optional[torch.Tensor] = None) -> dict:
+    """tslt_linear_ce: hidden [..., D] and weight [V, D] bf16, target [rows] int32 (negative: the row is ignored).
+    Returns dict(loss [rows], lse [rows] fp32, workspace), both 0 in ignored rows."""
+    dev, rows, V, D, hs, wstride = _loss_inputs(hidden, weight, target)
+    device = hidden.device
+    o = out if out is not None else {}
+    for name in ("loss", "lse"):
+        if name not in o:
+            o[name] = torch.empty(rows, dtype=torch.float32, device=device)
+        _vector(o[name], name, torch.float32, dev, rows)
+    ws = _space(ws, linear_ce_workspace_bytes(rows, V, D), device, dev)
+    _check(lib().tslt_linear_ce(_ptr(hidden), hs, _ptr(weight), wstride, _ptr(target), rows, V, D, _ptr(o["loss"]),
+                                _ptr(o["lse"]), _ptr(ws), ws.numel(), _stream()), "tslt_linear_ce")
+    o["workspace"] = ws
+    return o
+
+
+@_own_device
+def linear_ce_backward(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, lse: torch.Tensor,
+                       dloss: Optional[torch.Tensor] = None, *, out: Optional[dict] = None,
+                       ws: Optional[torch.Tensor] = None) -> dict:
+    """tslt_linear_ce_backward: lse as linear_ce wrote it, dloss [rows] fp32 the derivative of the caller's total by each
+    row's loss (None: 1, the sum of the losses; 1 / n in every row: their mean over n rows that count).  Returns
+    dict(dhidden [..., D], dweight [V, D] bf16, workspace).  The gradients are explicit: nothing is recorded by autograd."""
+    dev, rows, V, D, hs, wstride = _loss_inputs(hidden, weight, target)
+    device = hidden.device
+    _vector(lse, "lse", torch.float32, dev, rows)
+    if dloss is not None:
+        _vector(dloss, "dloss", torch.float32, dev, rows)
+    o = out if out is not None else {}
+    if "dhidden" not in o:
+        o["dhidden"] = _rows_like(hidden.shape[:-1], D, torch.bfloat16, device)
+    if "dweight" not in o:
+        o["dweight"] = _rows_like((V,), D, torch.bfloat16, device)
+    dr, _, dhs = _matrix(o["dhidden"], "dhidden", torch.bfloat16, dev, D)
+    dv, _, dws = _matrix(o["dweight"], "dweight", torch.bfloat16, dev, D)
+    if dr != rows or dv != V:
+        raise ValueError("output dhidden must have %d rows and dweight %d" % (rows, V))
+    ws = _space(ws, linear_ce_backward_workspace_bytes(rows, V, D), device, dev)
+    _check(lib().tslt_linear_ce_backward(_ptr(hidden), hs, _ptr(weight), wstride, _ptr(target), _ptr(lse), _ptr(dloss), rows, V, D,
+                                         _ptr(o["dhidden"]), dhs, _ptr(o["dweight"]), dws, _ptr(ws), ws.numel(), _stream()),
+           "tslt_linear_ce_backward")
     o["workspace"] = ws
     return o
