@@ -374,7 +374,8 @@ int tslt_diagnostics(const void* draft_logits, const void* target_logits, int dt
  * A row of zeros gives q = 0, scale = 0; a row with a NaN or an infinity gives a scale that is NaN.  (Sums of squares are
  * held in fp32: elements above about 1e17 overflow them, and the scale of such a row is 0.)
  * x, residual, weight and residual_out are TSLT_F32 or TSLT_BF16, all the same; residual and residual_out (which gets h) are
- * nullable; residual_out may be x or residual itself (same pointer and stride), no other overlap is allowed.
+ * nullable; residual_out may be x or residual itself (same pointer and stride), no other overlap is allowed.  values
+ * (nullable, bf16) gets q * scale, the rows that the codes stand for, for layers that are not held in 8 bits.
  * tslt_quantize_rows: the same quantiser without norm and weight (y = x): lays a head weight [V, D] out once for
  * tslt_head_logits, one scale per vocabulary entry.
  * Rows: x [rows, D] with a stride; q [rows, D] int8 with a stride; scale [rows] fp32.  Every base pointer 16-byte aligned,
@@ -382,7 +383,8 @@ int tslt_diagnostics(const void* draft_logits, const void* target_logits, int dt
  */
 int tslt_rmsnorm_quant(const void* x, const void* residual, const void* weight, int dtype, int rows, int D,
                        long long x_stride, long long residual_stride, float eps, void* residual_out,
-                       long long out_stride, signed char* q, long long q_stride, float* scale, void* stream);
+                       long long out_stride, void* values, long long values_stride, signed char* q,
+                       long long q_stride, float* scale, void* stream);
 int tslt_quantize_rows(const void* x, int dtype, int rows, int D, long long x_stride, signed char* q,
                        long long q_stride, float* scale, void* stream);
 

@@ -22,21 +22,21 @@ template <typename T> struct HeadEpilogue {
         *p = b;
     }
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int, int part) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int lane, int part) {
         const bool on = v < p.V;
         const float wv = on ? __ldg(p.weight_scale + v) : 0.f;
         const int n = min(t.nt, p.rows - t.col0);
         for (int c = part * 32; c < n; c += kParts * 32) {
             uint32_t r[32];
             gemm::tmem_ld32(tmem + c, r);
+            const float mine = c + lane < n ? __ldg(p.row_scale + t.col0 + c + lane) : 0.f;  // lane j: the scale of column c + j
             gemm::tmem_wait32(r);
             T* out = p.out + (long long)(t.col0 + c) * p.stride + v;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                if (c + j < n) {
-                    const float z = (float)(int)r[j] * __ldg(p.row_scale + t.col0 + c + j) * wv;  // left to right: s t alone could underflow
-                    if (on) put(out + j * p.stride, z);
-                }
+                // left to right: the product of the scales alone could underflow
+                const float z = (float)(int)r[j] * __shfl_sync(0xffffffffu, mine, j) * wv;
+                if (on && c + j < n) put(out + j * p.stride, z);
             }
         }
     }
@@ -64,7 +64,7 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
     if (!gemm::encode_map(&ta, true, w, K, V, w_stride, 128) || !gemm::encode_map(&tb, true, q, K, rows, q_stride, pair ? p.nt / 2 : p.nt))
         return TSLT_ERR_CUDA;
     const typename HeadEpilogue<T>::Params ep = {out, out_stride, qs, ws, rows, V};
-    return pair ? gemm::launch<true, 2, 4, HeadEpilogue<T>>(ta, tb, p, ep, st) : gemm::launch<true, 1, 4, HeadEpilogue<T>>(ta, tb, p, ep, st);
+    return pair ? gemm::launch<true, 2, 8, HeadEpilogue<T>>(ta, tb, p, ep, st) : gemm::launch<true, 1, 8, HeadEpilogue<T>>(ta, tb, p, ep, st);
 }
 
 }  // namespace tslt

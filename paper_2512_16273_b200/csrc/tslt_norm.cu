@@ -18,22 +18,26 @@ namespace tslt {
 struct NormParams {
     const void *x, *r, *w;  // r, w may be null
     void* h;                // may be null; may equal x or r
+    uint16_t* y;            // may be null: q * scale in bf16
     int8_t* q;
     float* scale;
-    long long xs, rs, hs, qs;  // row strides in elements
+    long long xs, rs, hs, ys, qs;  // row strides in elements
     int rows, D;
     float eps;
 };
 
-__device__ __forceinline__ int code_of(float v, float top, float inv) {
+// The code of v as a float.  Adding and taking away 1.5 * 2^23 rounds to the nearest integer, ties to even, at the rate of
+// an addition (the conversion instructions run at an eighth of it).
+constexpr float kRounder = 12582912.f;
+__device__ __forceinline__ float code_of(float v, float top, float inv) {
     const float t = v * inv;
-    float c = rintf(t);
+    float c = __fadd_rn(__fadd_rn(t, kRounder), -kRounder);
     // A NaN t (v or top not finite, or top so small that inv overflowed) fails the comparison too.
     if (!(fabsf(t - c) < 0.4999f)) {
         const double e = rint(127.0 * (double)v / (double)top);
         c = e == e ? fminf(fmaxf((float)e, -127.f), 127.f) : 0.f;
     }
-    return (int)c;
+    return c;
 }
 
 // fp32 -> storage type, round to nearest even (bf16 patterns built by hand would cost more than the conversion)
@@ -154,37 +158,48 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024) norm_
         sum += s_sum[w];
         top = fmaxf(top, s_top[w]);
     }
-    if (tid == 0) {
-        float s;
-        if (kNorm) {
-            const float rstd = (float)(1.0 / sqrt((double)sum / p.D + (double)p.eps));
-            s = top * rstd / 127.f;
-            if (top == 0.f && sum == sum) s = 0.f;
-        } else {
-            s = top / 127.f + sum;
-        }
-        p.scale[row] = s;
-    }
+    float s = top / 127.f;
+    if (kNorm) s = top == 0.f && sum == sum ? 0.f : s / sqrtf(sum / (float)p.D + p.eps);
+    else s += sum;
+    if (tid == 0) p.scale[row] = s;
     const float inv = top > 0.f ? 127.f / top : 0.f;
     int8_t* q = p.q + row * p.qs;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int at = (tid + j * nth) * P;
         if (at >= p.D) break;
-        uint32_t c[P / 4];
+        float c[P];
 #pragma unroll
-        for (int i = 0; i < P / 4; ++i) {
-            c[i] = 0;
+        for (int i = 0; i < P; ++i) c[i] = code_of(v[j][i], top, inv);
+        uint32_t b[P / 4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) c[i] |= ((uint32_t)code_of(v[j][4 * i + k], top, inv) & 0xffu) << (8 * k);
+        for (int i = 0; i < P / 4; ++i) {  // the low byte of c + kRounder is the code
+            uint32_t k[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[e] = __float_as_uint(__fadd_rn(c[4 * i + e], kRounder));
+            b[i] = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
         }
         if (at + P <= p.D) {
-            if (P == 8) *reinterpret_cast<uint2*>(q + at) = make_uint2(c[0], c[P / 4 - 1]);
-            else *reinterpret_cast<uint32_t*>(q + at) = c[0];
+            if (P == 8) *reinterpret_cast<uint2*>(q + at) = make_uint2(b[0], b[P / 4 - 1]);
+            else *reinterpret_cast<uint32_t*>(q + at) = b[0];
         } else {
 #pragma unroll
             for (int i = 0; i < P; ++i)
-                if (at + i < p.D) q[at + i] = (int8_t)(c[i / 4] >> (8 * (i % 4)));
+                if (at + i < p.D) q[at + i] = (int8_t)(b[i / 4] >> (8 * (i % 4)));
+        }
+        if (kNorm && p.y) {
+            uint16_t* y = p.y + row * p.ys + at;
+            uint32_t o[P / 2];
+#pragma unroll
+            for (int i = 0; i < P / 2; ++i) o[i] = pack_bf16x2(c[2 * i] * s, c[2 * i + 1] * s);
+            if (at + P <= p.D) {
+                if (P == 8) *reinterpret_cast<uint4*>(y) = make_uint4(o[0], o[1], o[P / 2 - 2], o[P / 2 - 1]);
+                else *reinterpret_cast<uint2*>(y) = make_uint2(o[0], o[1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+                    if (at + i < p.D) y[i] = (uint16_t)(o[i / 2] >> (16 * (i % 2)));
+            }
         }
     }
 }
@@ -195,7 +210,7 @@ template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cu
     const int nvec = (p.D + Elt<T>::kPerVec - 1) / Elt<T>::kPerVec;
     // Few rows: latency counts, so a row is spread over as many threads as it has vectors.  Rows enough to fill the
     // machine: several vectors in flight per thread.
-    int nv = p.rows < 2 * 148 ? 1 : (nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1);
+    int nv = p.rows < 2 * 148 ? 1 : (nvec >= 256 ? 2 : 1);
     while ((nvec + nv - 1) / nv > 1024) nv *= 2;
     const int threads = ((nvec + nv - 1) / nv + 31) / 32 * 32;
     if (nv == 1) norm_quant_kernel<T, 1, kNorm><<<p.rows, threads, 0, st>>>(p);
@@ -216,7 +231,8 @@ using namespace tslt;
 
 extern "C" int tslt_rmsnorm_quant(const void* x, const void* residual, const void* weight, int dtype, int rows, int D,
                                   long long x_stride, long long residual_stride, float eps, void* residual_out,
-                                  long long out_stride, signed char* q, long long q_stride, float* scale, void* stream) {
+                                  long long out_stride, void* values, long long values_stride, signed char* q, long long q_stride,
+                                  float* scale, void* stream) {
     if (dtype != TSLT_F32 && dtype != TSLT_BF16) return TSLT_ERR_UNSUPPORTED;
     if (rows < 0 || D <= 0 || !(eps >= 0.f)) return TSLT_ERR_INVALID_ARG;
     if (D > kMaxHidden) return TSLT_ERR_UNSUPPORTED;
@@ -225,9 +241,10 @@ extern "C" int tslt_rmsnorm_quant(const void* x, const void* residual, const voi
     if (!row_ok(x, x_stride, D, b) || !row_ok(q, q_stride, D, 1) || !scale) return TSLT_ERR_INVALID_ARG;
     if (residual && !row_ok(residual, residual_stride, D, b)) return TSLT_ERR_INVALID_ARG;
     if (residual_out && !row_ok(residual_out, out_stride, D, b)) return TSLT_ERR_INVALID_ARG;
+    if (values && !row_ok(values, values_stride, D, 2)) return TSLT_ERR_INVALID_ARG;
     if (weight && !aligned16(weight)) return TSLT_ERR_INVALID_ARG;
-    NormParams p = {x, residual, weight, residual_out, (int8_t*)q, scale, x_stride, residual_stride, out_stride, q_stride,
-                    rows, D, eps};
+    NormParams p = {x, residual, weight, residual_out, (uint16_t*)values, (int8_t*)q, scale, x_stride, residual_stride, out_stride,
+                    values_stride, q_stride, rows, D, eps};
     return dtype == TSLT_F32 ? launch_norm<float, true>(p, (cudaStream_t)stream)
                              : launch_norm<bf16_t, true>(p, (cudaStream_t)stream);
 }
@@ -239,7 +256,7 @@ extern "C" int tslt_quantize_rows(const void* x, int dtype, int rows, int D, lon
     if (D > kMaxHidden) return TSLT_ERR_UNSUPPORTED;
     if (rows == 0) return TSLT_OK;
     if (!row_ok(x, x_stride, D, elt_bytes(dtype)) || !row_ok(q, q_stride, D, 1) || !scale) return TSLT_ERR_INVALID_ARG;
-    NormParams p = {x, nullptr, nullptr, nullptr, (int8_t*)q, scale, x_stride, 0, 0, q_stride, rows, D, 0.f};
+    NormParams p = {x, nullptr, nullptr, nullptr, nullptr, (int8_t*)q, scale, x_stride, 0, 0, 0, q_stride, rows, D, 0.f};
     return dtype == TSLT_F32 ? launch_norm<float, false>(p, (cudaStream_t)stream)
                              : launch_norm<bf16_t, false>(p, (cudaStream_t)stream);
 }

@@ -105,7 +105,7 @@ def lib() -> ctypes.CDLL:
     L.tslt_unpack_payload.restype = i
     L.tslt_unpack_payload.argtypes = [p, i, i, i, i, p, p, p, p, p]
     L.tslt_rmsnorm_quant.restype = i
-    L.tslt_rmsnorm_quant.argtypes = [p, p, p, i, i, i, ll, ll, f, p, ll, p, ll, p, p]
+    L.tslt_rmsnorm_quant.argtypes = [p, p, p, i, i, i, ll, ll, f, p, ll, p, ll, p, ll, p, p]
     L.tslt_quantize_rows.restype = i
     L.tslt_quantize_rows.argtypes = [p, i, i, i, ll, p, ll, p, p]
     L.tslt_head_logits.restype = i
@@ -742,22 +742,33 @@ def _own_device(call):
     return on_device
 
 
-def _matrix(t, name: str, dtype, dev: int, cols: Optional[int] = None):
-    """(rows, columns, row stride) of a CUDA tensor [..., columns] on device `dev` with evenly spaced rows."""
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_on(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _check_tensor(t, name: str, dtype, dev: int) -> None:
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor (libtslt has no CPU path)" % name)
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s must have dtype %s" % (name, dtype))
     if t.get_device() != dev:
         raise ValueError("%s is on another device" % name)
-    if t.dim() == 2:
-        rows, c = t.shape
-        stride = t.stride(0)
-        if c > 1 and t.stride(1) != 1:
-            raise ValueError("%s must be contiguous along its last dimension" % name)
-        if rows > 1 and stride < c:
-            raise ValueError("rows of %s overlap" % name)
-    elif t.dim() < 1:
+
+
+def _matrix(t, name: str, dtype, dev: int, cols: Optional[int] = None):
+    """(rows, columns, row stride) of a CUDA tensor [..., columns] on device `dev` with evenly spaced rows."""
+    _check_tensor(t, name, dtype, dev)
+    shape = t.shape
+    if len(shape) == 2:
+        rows, c = shape
+        stride, inner = t.stride()
+        if (inner != 1 and c > 1) or (stride < c and rows > 1):
+            raise ValueError("rows of %s must be contiguous and must not overlap" % name)
+    elif not shape:
         raise ValueError("%s must have at least one dimension" % name)
     else:
         rows, c, stride = _row_layout(t)
@@ -771,23 +782,21 @@ def _matrix(t, name: str, dtype, dev: int, cols: Optional[int] = None):
 
 def _vector(t, name: str, dtype, dev: int, numel: int):
     """A contiguous CUDA tensor of numel elements on device `dev`."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError("%s must be a CUDA tensor (libtslt has no CPU path)" % name)
-    if t.dtype != dtype:
-        raise ValueError("%s must have dtype %s" % (name, dtype))
-    if t.get_device() != dev:
-        raise ValueError("%s is on another device" % name)
+    _check_tensor(t, name, dtype, dev)
     if t.numel() != numel or not t.is_contiguous():
         raise ValueError("%s must be contiguous with %d elements" % (name, numel))
     return t
 
 
+_STEP = {torch.float32: 4, torch.bfloat16: 8, torch.int8: 16}  # elements of 16 bytes
+
+
 def _rows_like(lead, cols: int, dtype, device) -> torch.Tensor:
     """An empty [*lead, cols] whose rows start on 16-byte boundaries."""
-    step = 16 // (torch.finfo(dtype).bits // 8 if dtype.is_floating_point else 1)
-    wide = -(-cols // step) * step
-    t = torch.empty(*lead, wide, dtype=dtype, device=device)
-    return t if wide == cols else t[..., :cols]
+    step = _STEP[dtype]
+    if cols % step == 0:
+        return torch.empty(*lead, cols, dtype=dtype, device=device)
+    return torch.empty(*lead, -(-cols // step) * step, dtype=dtype, device=device)[..., :cols]
 
 
 def _scratch(nbytes: int, device) -> torch.Tensor:
@@ -801,45 +810,52 @@ def _scratch(nbytes: int, device) -> torch.Tensor:
 def _space(ws, nbytes: int, device, dev: int) -> torch.Tensor:
     if ws is None:
         return _scratch(nbytes, device)
-    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or not ws.is_cuda or ws.get_device() != dev or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous uint8 CUDA tensor on the call's device")
+    _check_tensor(ws, "ws", torch.uint8, dev)
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
     return ws
 
 
 @_own_device
 def rmsnorm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
-                  eps: float = 1e-6, *, out: Optional[dict] = None) -> dict:
+                  eps: float = 1e-6, *, want_values: bool = False, out: Optional[dict] = None) -> dict:
     """tslt_rmsnorm_quant on hidden states x [..., D] (fp32 / bf16), weight [D] and residual [..., D] of the same type.
 
-    Returns dict(q [..., D] int8, scale [rows] fp32, and with a residual residual [..., D] = x + residual), q * scale
-    being the normalised rows.  `out` may hold any of them; out["residual"] may be x or residual itself."""
+    Returns dict(q [..., D] int8, scale [rows] fp32, with a residual residual [..., D] = x + residual, and with want_values
+    values [..., D] bf16 = q * scale, the normalised rows).  `out` may hold any of them; out["residual"] may be x or
+    residual itself."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("x must be a CUDA tensor (libtslt has no CPU path)")
-    code, dev, device = _dtype_code(x), x.get_device(), x.device
+    code, dev, device, shape = _dtype_code(x), x.get_device(), x.device, x.shape
     rows, D, xs = _matrix(x, "x", None, dev)
-    rs = hs = 0
+    rs = hs = vs = 0
     if residual is not None:
-        if residual.shape != x.shape:
+        if residual.shape != shape:
             raise ValueError("residual must have the shape of x")
         rs = _matrix(residual, "residual", x.dtype, dev, D)[2]
     if weight is not None:
         _vector(weight, "weight", x.dtype, dev, D)
     o = out if out is not None else {}
+    lead = shape[:-1]
     if "q" not in o:
-        o["q"] = _rows_like(x.shape[:-1], D, torch.int8, device)
+        o["q"] = _rows_like(lead, D, torch.int8, device)
     if "scale" not in o:
         o["scale"] = torch.empty(rows, dtype=torch.float32, device=device)
     if residual is not None and "residual" not in o:
-        o["residual"] = _rows_like(x.shape[:-1], D, x.dtype, device)
-    h = o.get("residual")
-    if o["q"].shape != x.shape or (h is not None and h.shape != x.shape):
-        raise ValueError("outputs q and residual must have the shape of x")
-    qs = _matrix(o["q"], "q", torch.int8, dev, D)[2]
+        o["residual"] = _rows_like(lead, D, x.dtype, device)
+    if want_values and "values" not in o:
+        o["values"] = _rows_like(lead, D, torch.bfloat16, device)
+    q, scale, h, y = o["q"], o["scale"], o.get("residual"), o.get("values")
+    if q.shape != shape or (h is not None and h.shape != shape) or (y is not None and y.shape != shape):
+        raise ValueError("outputs q, residual and values must have the shape of x")
+    qs = _matrix(q, "q", torch.int8, dev, D)[2]
     if h is not None:
         hs = _matrix(h, "output residual", x.dtype, dev, D)[2]
-    _vector(o["scale"], "scale", torch.float32, dev, rows)
-    _check(lib().tslt_rmsnorm_quant(_ptr(x), _ptr(residual), _ptr(weight), code, rows, D, xs, rs, eps, _ptr(h), hs,
-                                    _ptr(o["q"]), qs, _ptr(o["scale"]), _stream()), "tslt_rmsnorm_quant")
+    if y is not None:
+        vs = _matrix(y, "output values", torch.bfloat16, dev, D)[2]
+    _vector(scale, "scale", torch.float32, dev, rows)
+    _check(lib().tslt_rmsnorm_quant(_at(x), _at(residual), _at(weight), code, rows, D, xs, rs, eps, _at(h), hs, _at(y), vs,
+                                    _at(q), qs, _at(scale), _stream_on(dev)), "tslt_rmsnorm_quant")
     return o
 
 
@@ -860,7 +876,7 @@ def quantize_rows(x: torch.Tensor, *, out: Optional[dict] = None) -> dict:
         raise ValueError("output q must have the shape of x")
     qs = _matrix(o["q"], "q", torch.int8, dev, D)[2]
     _vector(o["scale"], "scale", torch.float32, dev, rows)
-    _check(lib().tslt_quantize_rows(_ptr(x), code, rows, D, xs, _ptr(o["q"]), qs, _ptr(o["scale"]), _stream()),
+    _check(lib().tslt_quantize_rows(_at(x), code, rows, D, xs, _at(o["q"]), qs, _at(o["scale"]), _stream_on(dev)),
            "tslt_quantize_rows")
     return o
 
@@ -891,8 +907,8 @@ def head_logits(q: torch.Tensor, scale: torch.Tensor, weight: torch.Tensor, weig
     if zr != rows:
         raise ValueError("output logits must have %d rows" % rows)
     ws = _space(ws, 256, device, dev)
-    _check(lib().tslt_head_logits(_ptr(q), _ptr(scale), qs, _ptr(weight), _ptr(weight_scale), wstride, rows, V, D,
-                                  F32 if logits_dtype == torch.float32 else BF16, _ptr(z), zs, _ptr(ws), ws.numel(), _stream()),
+    _check(lib().tslt_head_logits(_at(q), _at(scale), qs, _at(weight), _at(weight_scale), wstride, rows, V, D,
+                                  F32 if logits_dtype == torch.float32 else BF16, _at(z), zs, _at(ws), ws.numel(), _stream_on(dev)),
            "tslt_head_logits")
     o["workspace"] = ws
     return o
@@ -957,8 +973,8 @@ def linear_ce(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, 
             o[name] = torch.empty(rows, dtype=torch.float32, device=device)
         _vector(o[name], name, torch.float32, dev, rows)
     ws = _space(ws, linear_ce_workspace_bytes(rows, V, D), device, dev)
-    _check(lib().tslt_linear_ce(_ptr(hidden), hs, _ptr(weight), wstride, _ptr(target), rows, V, D, _ptr(o["loss"]),
-                                _ptr(o["lse"]), _ptr(ws), ws.numel(), _stream()), "tslt_linear_ce")
+    _check(lib().tslt_linear_ce(_at(hidden), hs, _at(weight), wstride, _at(target), rows, V, D, _at(o["loss"]),
+                                _at(o["lse"]), _at(ws), ws.numel(), _stream_on(dev)), "tslt_linear_ce")
     o["workspace"] = ws
     return o
 
@@ -985,8 +1001,8 @@ def linear_ce_backward(hidden: torch.Tensor, weight: torch.Tensor, target: torch
     if dr != rows or dv != V:
         raise ValueError("output dhidden must have %d rows and dweight %d" % (rows, V))
     ws = _space(ws, linear_ce_backward_workspace_bytes(rows, V, D), device, dev)
-    _check(lib().tslt_linear_ce_backward(_ptr(hidden), hs, _ptr(weight), wstride, _ptr(target), _ptr(lse), _ptr(dloss), rows, V, D,
-                                         _ptr(o["dhidden"]), dhs, _ptr(o["dweight"]), dws, _ptr(ws), ws.numel(), _stream()),
+    _check(lib().tslt_linear_ce_backward(_at(hidden), hs, _at(weight), wstride, _at(target), _at(lse), _at(dloss), rows, V, D,
+                                         _at(o["dhidden"]), dhs, _at(o["dweight"]), dws, _at(ws), ws.numel(), _stream_on(dev)),
            "tslt_linear_ce_backward")
     o["workspace"] = ws
     return o

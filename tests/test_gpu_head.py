@@ -64,12 +64,14 @@ def test_rmsnorm_quant(dtype, rows, D, residual):
             r[1] = 0
         x[2] *= 1e-3
     h, q, scale = norm_reference(x, r, w, 1e-6)
-    o = tslt.rmsnorm_quant(padded(x, 1), w, None if r is None else padded(r, 2), 1e-6)
+    o = tslt.rmsnorm_quant(padded(x, 1), w, None if r is None else padded(r, 2), 1e-6, want_values=True)
     if residual:
         assert torch.equal(o["residual"], h)
     assert torch.equal(o["q"].double(), q)
     # the sum of D squares in fp32 (relative D U32 at most, halved by the root), and a few roundings
     within(o["scale"], scale, scale * ((D / 2 + 8) * U32), "scale")
+    y = q * scale[:, None]  # the scale's error, the product and the rounding to bf16
+    within(o["values"], y, y.abs() * ((D / 2 + 10) * U32 + UBF * 1.01), "values")
 
 
 def test_rmsnorm_quant_leaves_padding_and_works_in_place():
