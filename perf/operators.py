@@ -155,10 +155,8 @@ def run(s):
 def _own(s):
     from paper_2512_16273_b200 import tslt
     if s["op"] == "norm":
-        o = tslt.rmsnorm_quant(s["x"], s["w"], s["r"], EPS)
-        values = torch.empty(o["q"].shape, dtype=torch.bfloat16, device="cuda")
-        torch.mul(o["q"], o["scale"][:, None], out=values)  # what the codes stand for
-        return [values, o["scale"], o["residual"]] if s["r"] is not None else [values, o["scale"]]
+        o = tslt.rmsnorm_quant(s["x"], s["w"], s["r"], EPS, want_values=True)
+        return [o["values"], o["scale"], o["residual"]] if s["r"] is not None else [o["values"], o["scale"]]
     if s["op"] == "head":
         return [tslt.head_logits(s["q"], s["qs"], s["w"], s["ws"], _TYPE[s["logits"]])["logits"]]
     f = tslt.linear_ce(s["h"], s["w"], s["t"])
