@@ -11,8 +11,10 @@
 // Roles.  Warp 0: TMA producer (one lane).  Warp 1: allocates tensor memory, issues the products (one lane of the
 // leader CTA).  The other warps: epilogue, warp w reading tensor-memory lanes 32 (w mod 4) ... + 31.
 //
-// Operands are K-major (k contiguous) or MN-major (m or n contiguous); out-of-range rows and columns of a copy read as
-// zero, so that ragged sizes need no special case before the epilogue.
+// Operands are K-major (k contiguous) or MN-major (m or n contiguous), each from a plain row-major matrix or from panels:
+// [columns / 64][rows][64], a matrix that this library laid out itself so that a 64-column box is contiguous memory (whole
+// DRAM pages and full lines, whichever way it is read).  Out-of-range rows and columns of a copy read as zero, so that
+// ragged sizes need no special case before the epilogue.
 //
 // Waits.  Every wait on a barrier is bounded (kWaitLimit polls).  One that runs out sets an abort flag in shared memory
 // and TSLT_STATUS_WAIT_TIMEOUT in the status word; every role then leaves its loop, copies in flight are waited for
@@ -40,7 +42,8 @@ struct Product {
     int m_tiles, n_tiles, splits;  // tiles of 128 * kCtas rows, of nt columns; cuts of k
     int k_blocks;                  // stages of k in all (128 bytes of k each when K-major, 64 elements when MN-major)
     int nt, stages, group_m;
-    int a_mn, b_mn;                // 1: MN-major
+    int a_layout, b_layout;        // Layout
+    int pitch;                     // rows of a panel (kPanelsK)
     int k_elems;                   // elements of k in a stage
     int m_total;                   // rows of A
     const int* m_limit;
@@ -104,6 +107,38 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
             "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
             "l"(map), "r"(x), "r"(y), "r"(bar)
             : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    if (kCtas == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+}
+// How an operand lies in memory, and so how a stage of it is copied.  Few large boxes: the copy engine's rate falls with the
+// number of instructions (stages of four 8 KB boxes instead of two of 16 KB: 570 instead of 390 us for the copies alone of
+// a 6144 x 16128 x 4096 product).
+enum Layout {
+    kRowsK = 0,    // row-major, k contiguous: box of 128 bytes of k by n rows
+    kPanelsK = 1,  // panels, k along the columns: the same box, contiguous memory
+    kBlocksMN = 2, // m (n) contiguous, seen as [64-column blocks][k][64]: one box for the whole stage.  Panels, or a row-major
+                   // matrix whose width is a multiple of 64
+    kRowsMN = 3,   // m (n) contiguous, row-major of any width: a box for each 64 columns
+};
+// A stage: `n` rows of the operand from mn0 on, 128 bytes of k (64 elements of it when m is contiguous) from k0 on.
+template <int kCtas>
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* map, int layout, int pitch, int mn0, int n, int k0, uint32_t bar) {
+    if (layout == kRowsK) tma_load<kCtas>(dst, map, k0, mn0, bar);
+    else if (layout == kPanelsK) tma_load<kCtas>(dst, map, 0, (k0 >> 6) * pitch + mn0, bar);
+    else if (layout == kBlocksMN) tma_load3<kCtas>(dst, map, 0, k0, mn0 >> 6, bar);
+    else
+        for (int j = 0; j < n; j += 64) tma_load<kCtas>(dst + j * 128, map, mn0 + j, k0, bar);
 }
 template <int kCtas> __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem) {
     if (kCtas == 2) {
@@ -289,17 +324,8 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
                     if (rank == 0) mbar_expect(bar, tx);
                     if (kCtas == 2) bar = map_to_rank(bar, 0);
                     const int k0 = kb * p.k_elems;
-                    if (p.a_mn) {
-                        tma_load<kCtas>(sa, &ta, t.row0, k0, bar);
-                        tma_load<kCtas>(sa + 8192, &ta, t.row0 + 64, k0, bar);
-                    } else {
-                        tma_load<kCtas>(sa, &ta, k0, t.row0, bar);
-                    }
-                    if (p.b_mn) {
-                        for (int j = 0; j < p.nt / kCtas; j += 64) tma_load<kCtas>(sb + j * 128, &tb, brow + j, k0, bar);
-                    } else {
-                        tma_load<kCtas>(sb, &tb, k0, brow, bar);
-                    }
+                    load_operand<kCtas>(sa, &ta, p.a_layout, p.pitch, t.row0, 128, k0, bar);
+                    load_operand<kCtas>(sb, &tb, p.b_layout, p.pitch, brow, p.nt / kCtas, k0, bar);
                     if (++stage == p.stages) {
                         stage = 0;
                         phase ^= 1;
@@ -324,7 +350,8 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
         if (lane == 0 && rank == 0) {
             int stage = 0, phase = 0, acc = 0, acc_phase = 0;
             bool ok = true;
-            const uint32_t a_step = p.a_mn ? 2048 >> 4 : 32 >> 4, b_step = p.b_mn ? 2048 >> 4 : 32 >> 4;
+            const bool a_mn = p.a_layout >= kBlocksMN, b_mn = p.b_layout >= kBlocksMN;
+            const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
             for (int idx = cluster; idx < walk.total && ok; idx += clusters) {
                 const Tile t = walk.at(p, idx, kTileRows, rank);
                 if (t.k_begin >= t.k_end) continue;  // nothing to add up: the epilogue takes zeros
@@ -338,7 +365,7 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
                     }
                     tc_fence_after();
                     const uint32_t sa = data + stage * stage_bytes;
-                    const uint64_t da = make_desc(sa, p.a_mn ? 8192 : 16), db = make_desc(sa + kStageA, p.b_mn ? 8192 : 16);
+                    const uint64_t da = make_desc(sa, a_mn ? 8192 : 16), db = make_desc(sa + kStageA, b_mn ? 8192 : 16);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         mma<kCtas, kInt8>(d, da + j * a_step, db + j * b_step, p.idesc, kb > t.k_begin || j > 0);
@@ -393,6 +420,8 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
 // ---- host --------------------------------------------------------------------------------------------------
 // A 2-d tensor map of `outer` rows of `inner` elements (row stride in bytes, a multiple of 16), boxes of box_inner x
 // box_outer with box_inner elements = 128 bytes.
+// encode_blocks: bf16 as [blocks][rows][64] (kBlocksMN), boxes of box_blocks x 64 x 64; strides in bytes.
+bool encode_blocks(CUtensorMap* map, const void* base, long long rows, long long row_bytes, long long blocks, long long block_bytes, int box_blocks);
 bool encode_map(CUtensorMap* map, bool int8, const void* base, long long inner, long long outer, long long row_bytes, int box_outer);
 
 inline int sm_count() {  // of the current device; 0 if it cannot be found out
@@ -419,7 +448,7 @@ int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typena
     const int stage = kStageA + p.nt / kCtas * 128;
     p.stages = (kSmemLimit - 1024 - kBarrierBytes) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
-    p.idesc = instruction_desc(kInt8, 128 * kCtas, p.nt, p.a_mn != 0, p.b_mn != 0);
+    p.idesc = instruction_desc(kInt8, 128 * kCtas, p.nt, p.a_layout >= kBlocksMN, p.b_layout >= kBlocksMN);
     auto kern = gemm_kernel<kInt8, kCtas, kEpiWarps, Epi>;
     const int smem = 1024 + kBarrierBytes + p.stages * stage;
     static bool done[64] = {};

@@ -4,10 +4,10 @@
 // Mathematics.  z = H W^T; lse_n = ln sum_v exp z[n, v]; loss_n = lse_n - z[n, t_n].  With g_n the weight of row n's loss,
 // G[n, v] = g_n (exp(z[n, v] - lse_n) - [v = t_n]), dH = G W, dW = G^T H.
 //
-// Forward: one product whose epilogue turns each 256-column tile of z, still in tensor memory, into a running (max, sum)
+// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way.  One product whose epilogue turns each 256-column tile of z, still in tensor memory, into a running (max, sum)
 // pair per row; the pairs of all tiles (8 bytes for 256 logits) go to the workspace and a small kernel joins them.
 // Backward, piece by piece of the vocabulary: z of the piece is computed again and its epilogue writes G of the piece in
-// bf16 to the workspace; two products read it, dW of the piece (complete: its sum runs over the rows) and the piece's part
+// bf16 to the workspace (as 64-column panels, contiguous whichever of its axes a product reads along); two products read it, dW of the piece (complete: its sum runs over the rows) and the piece's part
 // of dH (summed over the pieces in fp32, in a fixed order).  Bound by the tensor cores: 2 + 6 products of rows x V x D
 // multiply-adds (the recomputation is the price of not keeping rows x V logits).
 //
@@ -20,6 +20,7 @@ namespace tslt {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
+constexpr int kStatsParts = 2;                         // (max, sum) pairs a row and tile: column halves of the epilogue
 constexpr int kTileN = 256;                            // vocabulary entries (or hidden units) of a tile
 constexpr long long kPieceBytes = 256ll << 20;         // most bytes of G held at a time
 
@@ -32,13 +33,14 @@ struct CeSpace {
     int* count;
     int* row_of;       // [rows_pad] source row of the i-th row that counts
     int* target;       // [rows_pad]
+    float* top_weight; // the largest |g| of the rows that count          (backward)
     float* lse2;       // [rows_pad] lse * log2(e)                        (backward)
-    float* weight;     // [rows_pad] g                                    (backward)
-    uint16_t* hidden;  // [rows_pad, ds] the rows that count, bf16; zeros up to the next multiple of 256 rows
-    float2* part;      // [tiles, rows_pad] (max, sum) in base 2          (forward)
+    float* weight;     // [rows_pad] g / top_weight                       (backward)
+    uint16_t* hidden;  // panels [ds / 64][rows_pad][64]: the rows that count, bf16; zeros up to the next multiple of 256 rows
+    float2* part;      // [parts, rows_pad] (max, sum) in base 2          (forward)
     float* ztarget;    // [rows_pad]                                      (forward)
-    uint16_t* g;       // [rows_pad, piece]                               (backward)
-    float* acc;        // [splits, rows_pad, da]                          (backward)
+    uint16_t* g;       // panels [piece / 64][rows_pad][64]               (backward)
+    float* acc;        // [splits][da / 4][rows_pad][4]                   (backward)
     long long rows_pad, ds, da, tiles, piece;
     int pieces, splits, pair;
     size_t bytes;
@@ -57,12 +59,24 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     s.pieces = (int)((vt + c - 1) / c);
     s.piece = up((vt + s.pieces - 1) / s.pieces, kTileN);
     s.pieces = (int)((vt + s.piece - 1) / s.piece);
-    // dH of few rows has few tiles and a long sum: cut it so that the machine is full, 256 vocabulary entries a cut at least
-    const long long tile_rows = s.pair ? 256 : 128;
-    const long long tiles3 = up(rows, tile_rows) / tile_rows * (up(D, kTileN) / kTileN), slots = s.pair ? 74 : 148;
-    long long cuts = slots / tiles3;
-    if (cuts > s.piece / 256) cuts = s.piece / 256;
-    s.splits = (int)(cuts < 1 ? 1 : cuts);
+    // dH: cut its sum over the piece so that the last round of tiles wastes little.  How many rows count is only known on
+    // the device: the rule averages over all of them and three quarters, and charges 1.5 % for each further buffer.  Few
+    // rows have few tiles and a long sum: there, as many cuts as fill the machine.
+    const long long tile_rows = s.pair ? 256 : 128, slots = s.pair ? 74 : 148, cols = up(D, kTileN) / kTileN;
+    const long long m_all = up(rows, tile_rows) / tile_rows, m_less = up((rows * 3ll + 3) / 4, tile_rows) / tile_rows;
+    auto waste = [&](long long tiles, long long cuts) { return (double)(up(tiles * cuts, slots)) / (double)(tiles * cuts); };
+    long long most = slots / (m_all * cols);
+    if (most < 8) most = 8;
+    if (most > s.piece / 512) most = s.piece / 512;  // 8 stages a cut at least
+    s.splits = 1;
+    double best = 1e30;
+    for (long long c = 1; c <= most; ++c) {
+        const double cost = (waste(m_all * cols, c) + waste(m_less * cols, c)) * 0.5 + 0.015 * (double)c * (double)(m_all * cols) / slots;
+        if (cost < best) {
+            best = cost;
+            s.splits = (int)c;
+        }
+    }
     uint8_t* p = (uint8_t*)ws;
     size_t at = kWsHeaderBytes;
     auto take = [&](size_t n) {
@@ -72,6 +86,7 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     };
     s.status = (int*)p;
     s.count = (int*)(p + 128);
+    s.top_weight = (float*)(p + 132);
     s.row_of = (int*)take(s.rows_pad * 4);
     s.target = (int*)take(s.rows_pad * 4);
     s.hidden = (uint16_t*)take(s.rows_pad * s.ds * 2);
@@ -81,7 +96,7 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
         s.g = (uint16_t*)take(s.rows_pad * s.piece * 2);
         s.acc = (float*)take((size_t)s.splits * s.rows_pad * s.da * 4);
     } else {
-        s.part = (float2*)take(s.tiles * s.rows_pad * 8);
+        s.part = (float2*)take(s.tiles * kStatsParts * s.rows_pad * 8);
         s.ztarget = (float*)take(s.rows_pad * 4);
     }
     s.bytes = at;
@@ -90,10 +105,10 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
 
 // ---- gathering the rows that count --------------------------------------------------------------------------
 struct GatherParams {
-    const uint16_t* hidden;
+    const uint16_t *hidden, *weight;
     const int* target;
-    long long h_stride;
-    int rows, V, D;
+    long long h_stride, w_stride;
+    int rows, V, D, per;
     const float *lse_in, *weight_in;  // backward (weight_in may be null: 1)
     float *loss, *lse;                // forward: zeroed for ignored rows
     uint16_t* dhidden;                // backward: zeroed for ignored rows
@@ -104,66 +119,110 @@ constexpr int kGatherThreads = 256;
 
 __device__ __forceinline__ bool counts(int t, int V) { return t >= 0 && t < V; }
 
-__device__ __forceinline__ void copy_row(uint16_t* dst, const uint16_t* src, int D, int tid) {
-    const int vecs = D / 8;
-    for (int i = tid; i < vecs; i += kGatherThreads)
-        reinterpret_cast<uint4*>(dst)[i] = src ? reinterpret_cast<const uint4*>(src)[i] : make_uint4(0, 0, 0, 0);
-    for (int i = vecs * 8 + tid; i < D; i += kGatherThreads) dst[i] = src ? src[i] : (uint16_t)0;
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float acc) {
+    float x[8], y[8];
+    unpack_vec<bf16_t>(a, x);
+    unpack_vec<bf16_t>(b, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc = fmaf(x[i], y[i], acc);
+    return acc;
+}
+// The vector of elements [8 i, 8 i + 8) of a row of D, zeros past its end.
+__device__ __forceinline__ uint4 row_vec(const uint16_t* row, int i, int D) {
+    if (8 * i + 8 <= D) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int e = 8 * i + 2 * j;
+        w[j] = (e < D ? (uint32_t)row[e] : 0u) | (e + 1 < D ? (uint32_t)row[e + 1] << 16 : 0u);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// CTA b takes `per` source rows from b * per on: it counts the rows that count before them (and in all) from the targets,
-// which every CTA reads whole (they are few bytes next to the rows), so that no CTA waits for another.
-__global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_constant__ GatherParams p, int per) {
+// One warp per row, 8 rows of a CTA at a time; CTA b takes `per` source rows from b * per on.  How many rows count before
+// them (and in all) every CTA finds from the targets itself (few bytes next to the rows), so that none waits for another.
+__global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_constant__ GatherParams p) {
     __shared__ int s_before, s_all;
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int first = min(p.rows, (int)blockIdx.x * per), last = min(p.rows, first + per);
-    if (tid == 0) s_before = s_all = 0;
+    __shared__ uint32_t s_top;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int first = min(p.rows, (int)blockIdx.x * p.per), last = min(p.rows, first + p.per);
+    if (tid == 0) {
+        s_before = s_all = 0;
+        s_top = 0u;
+    }
     __syncthreads();
     int before = 0, all = 0, bad = 0;
+    float top = 0.f;
+#pragma unroll 8
     for (int i = tid; i < p.rows; i += kGatherThreads) {
-        const int t = p.target[i];
+        const int t = __ldg(p.target + i);
         const int c = counts(t, p.V);
         bad |= t >= p.V;
         all += c;
         before += i < first ? c : 0;
+        if (p.weight_in && c) top = fmaxf(top, fabsf(__ldg(p.weight_in + i)));
     }
     before = __reduce_add_sync(0xffffffffu, before);
     all = __reduce_add_sync(0xffffffffu, all);
+    top = warp_max(top);
     bad = __syncthreads_or(bad);
     if (lane == 0) {
         atomicAdd(&s_before, before);
         atomicAdd(&s_all, all);
+        atomicMax(&s_top, __float_as_uint(top));  // non-negative floats order as integers
     }
     __syncthreads();
-    int at = s_before;
+    const float wtop = p.weight_in ? __uint_as_float(s_top) : 1.f;
     if (blockIdx.x == 0 && tid == 0) {
         *p.s.status = bad ? TSLT_STATUS_BAD_TARGET : 0;
         *p.s.count = s_all;
+        *p.s.top_weight = wtop;
     }
-    for (int row = first; row < last; ++row) {
-        const int t = p.target[row];
-        if (counts(t, p.V)) {
-            copy_row(p.s.hidden + at * p.s.ds, p.hidden + row * p.h_stride, p.D, tid);
-            if (tid == 0) {
-                p.s.row_of[at] = row;
-                p.s.target[at] = t;
-                if (p.lse_in) {
-                    p.s.lse2[at] = (float)((double)p.lse_in[row] * 1.4426950408889634);
-                    p.s.weight[at] = p.weight_in ? p.weight_in[row] : 1.f;
+    const int vecs = (int)(p.s.ds / 8);
+    int at0 = s_before;
+    for (int r0 = first; r0 < last; r0 += 32) {  // 32 rows: a ballot gives each its place
+        const int mine = r0 + lane < last ? __ldg(p.target + r0 + lane) : -1;
+        const uint32_t on = __ballot_sync(0xffffffffu, counts(mine, p.V));
+        for (int j = warp; j < 32 && r0 + j < last; j += kGatherThreads / 32) {
+            const int row = r0 + j, t = __shfl_sync(0xffffffffu, mine, j);
+            if (on >> j & 1) {
+                const int at = at0 + __popc(on & ((1u << j) - 1u));
+                const uint16_t *h = p.hidden + row * p.h_stride, *w = p.weight + t * p.w_stride;
+                uint4* dst = reinterpret_cast<uint4*>(p.s.hidden) + (size_t)at * 8;
+                float z = 0.f;
+#pragma unroll 4
+                for (int i = lane; i < vecs; i += 32) {
+                    const uint4 v = row_vec(h, i, p.D);
+                    if (p.loss) z = dot8(v, row_vec(w, i, p.D), z);
+                    dst[(size_t)(i >> 3) * p.s.rows_pad * 8 + (i & 7)] = v;
                 }
+                if (p.loss) z = warp_sum(z);
+                if (lane == 0) {
+                    p.s.row_of[at] = row;
+                    p.s.target[at] = t;
+                    if (p.loss) {
+                        p.s.ztarget[at] = z;
+                    } else {
+                        p.s.lse2[at] = (float)((double)p.lse_in[row] * 1.4426950408889634);
+                        p.s.weight[at] = !p.weight_in ? 1.f : wtop > 0.f ? __fdiv_rn(p.weight_in[row], wtop) : 0.f;
+                    }
+                }
+            } else if (p.loss) {
+                if (lane == 0) p.loss[row] = p.lse[row] = 0.f;
+            } else {
+                uint16_t* o = p.dhidden + row * p.dh_stride;
+                for (int i = lane; i < p.D / 8; i += 32) reinterpret_cast<uint4*>(o)[i] = make_uint4(0, 0, 0, 0);
+                for (int i = p.D / 8 * 8 + lane; i < p.D; i += 32) o[i] = 0;
             }
-            ++at;
-        } else {
-            if (tid == 0 && p.loss) {
-                p.loss[row] = 0.f;
-                p.lse[row] = 0.f;
-            }
-            if (p.dhidden) copy_row(p.dhidden + row * p.dh_stride, nullptr, p.D, tid);
         }
+        at0 += __popc(on);
     }
     // zeros behind the last row: the products over rows run in steps of 64
     const int end = (s_all + 255) / 256 * 256;
-    for (int row = s_all + blockIdx.x; row < end; row += gridDim.x) copy_row(p.s.hidden + row * p.s.ds, nullptr, p.D, tid);
+    for (int row = s_all + blockIdx.x * (kGatherThreads / 32) + warp; row < end; row += gridDim.x * (kGatherThreads / 32)) {
+        uint4* dst = reinterpret_cast<uint4*>(p.s.hidden) + (size_t)row * 8;
+        for (int i = lane; i < vecs; i += 32) dst[(size_t)(i >> 3) * p.s.rows_pad * 8 + (i & 7)] = make_uint4(0, 0, 0, 0);
+    }
 }
 
 // ---- epilogues ---------------------------------------------------------------------------------------------
@@ -183,7 +242,7 @@ __device__ __forceinline__ float pick_column(uint32_t tmem, int col, int lane) {
 struct StatsEpilogue {
     struct Params {
         float2* part;
-        float* ztarget;
+        const float* ztarget;
         const int* target;
         long long rows_pad;
         int V;
@@ -214,14 +273,14 @@ struct StatsEpilogue {
             for (int j = 0; j < 32; ++j) add[j & 3] += ex2_approx(fmaf(__uint_as_float(r[j]), kLog2e, -m));
             s += (add[0] + add[1]) + (add[2] + add[3]);
         }
+        // The target's logit is known better than the tensor cores sum it (their additions truncate: a bias of some 1e-6 of a
+        // large logit), and it is often most of the row's sum: put the better value in its place.
         const bool on = row < t.rows;
+        const int col = on ? __ldg(p.target + row) - t.col0 : -1;
+        const bool here = col >= 0 && col < n && (col / 32) % kParts == part;
+        const float z = pick_column(tmem, here ? col : -1, lane);
+        if (here) s += ex2_approx(fmaf(__ldg(p.ztarget + row), kLog2e, -m)) - ex2_approx(fmaf(z, kLog2e, -m));
         if (on) p.part[((long long)t.n * kParts + part) * p.rows_pad + row] = make_float2(m, s);
-        if (part == 0) {
-            const int col = on ? __ldg(p.target + row) - t.col0 : -1;
-            const bool here = col >= 0 && col < n;
-            const float z = pick_column(tmem, here ? col : -1, lane);
-            if (here) p.ztarget[row] = z;
-        }
     }
 };
 
@@ -230,7 +289,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
         uint16_t* g;
         const float *lse2, *weight;
         const int* target;
-        long long stride;
+        long long rows_pad;
         int v0, n_real;  // first vocabulary entry of the piece; its entries
     };
     template <int kParts>
@@ -239,7 +298,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
         const float lse2 = on ? __ldg(p.lse2 + row) : 0.f, w = on ? __ldg(p.weight + row) : 0.f;
         const int col = on ? __ldg(p.target + row) - p.v0 - t.col0 : -1;
         const int n = min(t.nt, p.n_real - t.col0);
-        uint16_t* out = p.g + row * p.stride + t.col0;
+        auto at = [&](int c) { return p.g + ((long long)((t.col0 + c) >> 6) * p.rows_pad + row) * 64 + ((t.col0 + c) & 63); };
         for (int c = part * 32; c < t.nt; c += kParts * 32) {
             uint32_t r[32];
             gemm::tmem_ld32(tmem + c, r);
@@ -255,7 +314,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                reinterpret_cast<uint4*>(out + c)[j] = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
+                reinterpret_cast<uint4*>(at(c))[j] = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
         }
         // the target's entry, by the part that wrote its column
         const bool here = col >= 0 && col < n && (col / 32) % kParts == part;
@@ -263,7 +322,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
         if (here) {
             uint16_t b;
             asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"((ex2_approx(fmaf(z, kLog2e, -lse2)) - 1.f) * w));
-            out[col] = b;
+            *at(col) = b;
         }
     }
 };
@@ -271,35 +330,43 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
 struct WeightEpilogue {  // dW of a piece: rows are vocabulary entries
     struct Params {
         uint16_t* out;  // of the piece's first entry
+        const float* scale;
         long long stride;
-        int n_real, D;
+        int n_real, D, wide;  // wide: rows start on 32-byte boundaries
     };
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part) {
         const bool on = row < p.n_real;
+        const float scale = __ldg(p.scale);
         uint16_t* out = p.out + row * p.stride;
         for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
             uint32_t r[32];
             gemm::tmem_ld32(tmem + c, r);
             gemm::tmem_wait32(r);
-            if (zero) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) r[j] = 0;
-            }
             uint32_t b[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[j]) : "f"(__uint_as_float(r[2 * j + 1])), "f"(__uint_as_float(r[2 * j])));
+            for (int j = 0; j < 16; ++j) {
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[j]) : "f"(__uint_as_float(r[2 * j + 1]) * scale), "f"(__uint_as_float(r[2 * j]) * scale));
+                if (zero) b[j] = 0;
+            }
             const int d = t.col0 + c;
             if (on) {
+                if (p.wide && d + 32 <= p.D) {  // whole sectors
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (d + 8 * j + 8 <= p.D) {
-                        *reinterpret_cast<uint4*>(out + d + 8 * j) = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
-                    } else {
+                    for (int j = 0; j < 2; ++j)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + d + 16 * j), "r"(b[8 * j]), "r"(b[8 * j + 1]),
+                                     "r"(b[8 * j + 2]), "r"(b[8 * j + 3]), "r"(b[8 * j + 4]), "r"(b[8 * j + 5]), "r"(b[8 * j + 6]), "r"(b[8 * j + 7])
+                                     : "memory");
+                } else {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (d + 8 * j + i < p.D) out[d + 8 * j + i] = (uint16_t)(b[4 * j + i / 2] >> (16 * (i & 1)));
+                    for (int j = 0; j < 4; ++j) {
+                        if (d + 8 * j + 8 <= p.D) {
+                            *reinterpret_cast<uint4*>(out + d + 8 * j) = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                if (d + 8 * j + i < p.D) out[d + 8 * j + i] = (uint16_t)(b[4 * j + i / 2] >> (16 * (i & 1)));
+                        }
                     }
                 }
             }
@@ -307,35 +374,37 @@ struct WeightEpilogue {  // dW of a piece: rows are vocabulary entries
     }
 };
 
-struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer per cut of the sum)
+struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer per cut of the sum), laid out so that a warp's rows are adjacent
     struct Params {
-        float* acc;
+        float4* acc;
         long long rows_pad, da;
         int D, first;
     };
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part) {
         const bool on = row < t.rows;
-        float* out = p.acc + ((long long)t.split * p.rows_pad + row) * p.da;
         for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
             uint32_t r[32];
             gemm::tmem_ld32(tmem + c, r);
-            gemm::tmem_wait32(r);
             const int d = t.col0 + c;
+            float4* out = p.acc + (t.split * (p.da / 4) + d / 4) * p.rows_pad + row;
+            float4 a[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                a[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!p.first && on && d + 4 * j < p.D) a[j] = out[j * p.rows_pad];
+            }
+            gemm::tmem_wait32(r);
             if (on) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (d + 4 * j < p.D) {  // da is a multiple of 4: the vector stays inside the row
-                        float4* o = reinterpret_cast<float4*>(out + d + 4 * j);
-                        float4 v = zero ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                        : make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]),
-                                                      __uint_as_float(r[4 * j + 3]));
-                        if (!p.first) {
-                            const float4 a = *o;
-                            v = make_float4(a.x + v.x, a.y + v.y, a.z + v.z, a.w + v.w);
-                        }
-                        *o = v;
+                    if (!zero) {
+                        a[j].x += __uint_as_float(r[4 * j]);
+                        a[j].y += __uint_as_float(r[4 * j + 1]);
+                        a[j].z += __uint_as_float(r[4 * j + 2]);
+                        a[j].w += __uint_as_float(r[4 * j + 3]);
                     }
+                    if (d + 4 * j < p.D) out[j * p.rows_pad] = a[j];
                 }
             }
         }
@@ -343,79 +412,87 @@ struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer p
 };
 
 // ---- small kernels -----------------------------------------------------------------------------------------
-// Joins the tiles' (max, sum) pairs: a CTA takes 32 rows, its warps the tiles in turn; fp64 sums.
-constexpr int kJoinWarps = 16;
+// Joins the tiles' (max, sum) pairs: a CTA takes 32 rows, its warps the tiles in turn; fp64 sums, a fixed order.
+constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps) ce_join_kernel(CeSpace s, int parts, float* __restrict__ loss, float* __restrict__ lse) {
     __shared__ float s_m[kJoinWarps][32];
     __shared__ double s_s[kJoinWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x * 32 + lane, rows = *s.count;
+    if ((int)blockIdx.x * 32 >= rows) return;
+    const float2* at = s.part + (row < rows ? row : 0);
     float m = -INFINITY;
-    double sum = 0.0;
-    if (row < rows) {
-        for (int t = warp; t < parts; t += kJoinWarps) {
-            const float2 v = s.part[t * s.rows_pad + row];
-            if (v.x > m) {
-                sum = sum * (double)ex2_approx(m - v.x) + (double)v.y;
-                m = v.x;
-            } else {
-                sum += (double)(v.y * ex2_approx(v.x - m));
-            }
-        }
-    }
+#pragma unroll 8
+    for (int t = warp; t < parts; t += kJoinWarps) m = fmaxf(m, at[t * s.rows_pad].x);
     s_m[warp][lane] = m;
+    __syncthreads();
+    m = s_m[0][lane];
+    for (int w = 1; w < kJoinWarps; ++w) m = fmaxf(m, s_m[w][lane]);
+    double sum = 0.0;
+#pragma unroll 8
+    for (int t = warp; t < parts; t += kJoinWarps) {
+        const float2 v = at[t * s.rows_pad];
+        sum += (double)(v.y * ex2_approx(v.x - m));
+    }
     s_s[warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && row < rows) {
-        float top = s_m[0][lane];
-        for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, s_m[w][lane]);
         double all = 0.0;
-        for (int w = 0; w < kJoinWarps; ++w)
-            if (s_s[w][lane] != 0.0) all += s_s[w][lane] * exp2((double)s_m[w][lane] - (double)top);
-        const double l = kLn2 * ((double)top + log2(all));
+        for (int w = 0; w < kJoinWarps; ++w) all += s_s[w][lane];
+        const double l = kLn2 * ((double)m + log2(all));
         const int src = s.row_of[row];
         lse[src] = (float)l;
         loss[src] = (float)(l - (double)s.ztarget[row]);
     }
 }
 
-// dH: adds the cuts of the sum in order and puts the rows back in their places.
+// dH: adds the cuts of the sum in order and puts the rows back in their places, times the largest weight.  A CTA takes 32 rows
+// by 64 hidden units: read as they lie (rows adjacent), turned in shared memory, written as 128-byte pieces of rows.
 __global__ void __launch_bounds__(256) ce_scatter_kernel(CeSpace s, uint16_t* __restrict__ out, long long stride, int D) {
-    const int rows = *s.count;
-    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-        uint16_t* o = out + s.row_of[row] * stride;
-        const float* a = s.acc + (long long)row * s.da;
-        for (int d = threadIdx.x * 4; d < D; d += 1024) {
-            float4 v = *reinterpret_cast<const float4*>(a + d);
+    __shared__ uint32_t tile[32][33];
+    const int rows = *s.count, r0 = blockIdx.x * 32, d0 = blockIdx.y * 64;
+    if (r0 >= rows) return;
+    const float scale = *s.top_weight;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float4* acc = reinterpret_cast<const float4*>(s.acc);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c4 = warp + 8 * k, d = d0 + 4 * c4;
+        if (d < D && r0 + lane < rows) {
+            const float4* a = acc + (long long)(d / 4) * s.rows_pad + r0 + lane;
+            float4 v = *a;
             for (int i = 1; i < s.splits; ++i) {
-                const float4 w = *reinterpret_cast<const float4*>(a + i * s.rows_pad * s.da + d);
+                const float4 w = a[i * (s.da / 4) * s.rows_pad];
                 v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
             }
-            uint32_t lo, hi;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(v.y), "f"(v.x));
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(v.w), "f"(v.z));
-            if (d + 4 <= D) {
-                *reinterpret_cast<uint2*>(o + d) = make_uint2(lo, hi);
-            } else {
-                o[d] = (uint16_t)lo;
-                if (d + 1 < D) o[d + 1] = (uint16_t)(lo >> 16);
-                if (d + 2 < D) o[d + 2] = (uint16_t)hi;
-            }
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(tile[lane][2 * c4]) : "f"(v.y * scale), "f"(v.x * scale));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(tile[lane][2 * c4 + 1]) : "f"(v.w * scale), "f"(v.z * scale));
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = warp + 8 * k, d = d0 + 2 * lane;
+        if (r0 + r < rows && d < D) {
+            uint16_t* o = out + s.row_of[r0 + r] * stride + d;
+            const uint32_t v = tile[r][lane];
+            if (d + 1 < D) *reinterpret_cast<uint32_t*>(o) = v;
+            else *o = (uint16_t)v;
         }
     }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------
-static int gather(const GatherParams& p, cudaStream_t st) {
-    const int per = p.rows > 148 * 4 ? (p.rows + 148 * 4 - 1) / (148 * 4) : 1;
-    const int grid = (p.rows + per - 1) / per;
-    ce_gather_kernel<<<grid, kGatherThreads, 0, st>>>(p, per);
+static int gather(GatherParams p, cudaStream_t st) {
+    p.per = p.rows > 8 * 148 * 8 ? (p.rows + 148 * 8 - 1) / (148 * 8) : 8;
+    const int grid = (p.rows + p.per - 1) / p.per;
+    ce_gather_kernel<<<grid, kGatherThreads, 0, st>>>(p);
     return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
 }
 
-template <class Epi>
+template <class Epi, int kWarps>
 static int product(bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const gemm::Product& p, const typename Epi::Params& ep, cudaStream_t st) {
-    return pair ? gemm::launch<false, 2, 4, Epi>(ta, tb, p, ep, st) : gemm::launch<false, 1, 4, Epi>(ta, tb, p, ep, st);
+    return pair ? gemm::launch<false, 2, kWarps, Epi>(ta, tb, p, ep, st) : gemm::launch<false, 1, kWarps, Epi>(ta, tb, p, ep, st);
 }
 
 // z of `width` vocabulary entries from row v0 of the weight: the product that forward and backward share.
@@ -433,7 +510,9 @@ static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, 
     p->m_total = rows;
     p->m_limit = s.count;
     p->status = s.status;
-    return gemm::encode_map(ta, false, s.hidden, D, s.rows_pad, s.ds * 2, 128) &&
+    p->a_layout = gemm::kPanelsK;
+    p->pitch = (int)s.rows_pad;
+    return gemm::encode_map(ta, false, s.hidden, 64, s.ds / 64 * s.rows_pad, 128, 128) &&
                    gemm::encode_map(tb, false, w, D, width, w_stride * 2, s.pair ? kTileN / 2 : kTileN)
                ? TSLT_OK
                : TSLT_ERR_CUDA;
@@ -483,11 +562,12 @@ extern "C" int tslt_linear_ce(const void* hidden, long long hidden_stride, const
     gemm::Product p;
     CUtensorMap ta, tb;
     if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, &p, &ta, &tb)) return rc;
-    GatherParams g = {(const uint16_t*)hidden, target, hidden_stride, rows, V, D, nullptr, nullptr, loss, lse, nullptr, 0, s};
+    const GatherParams g = {(const uint16_t*)hidden, (const uint16_t*)weight, target, hidden_stride, weight_stride, rows, V, D, 0, nullptr,
+                            nullptr, loss, lse, nullptr, 0, s};
     if (const int rc = gather(g, st)) return rc;
     const StatsEpilogue::Params ep = {s.part, s.ztarget, s.target, s.rows_pad, V};
-    if (const int rc = product<StatsEpilogue>(s.pair, ta, tb, p, ep, st)) return rc;
-    ce_join_kernel<<<(rows + 31) / 32, 32 * kJoinWarps, 0, st>>>(s, (int)s.tiles, loss, lse);
+    if (const int rc = product<StatsEpilogue, 4 * kStatsParts>(s.pair, ta, tb, p, ep, st)) return rc;
+    ce_join_kernel<<<(rows + 31) / 32, 32 * kJoinWarps, 0, st>>>(s, (int)s.tiles * kStatsParts, loss, lse);
     return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
 }
 
@@ -505,7 +585,8 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
     if (bad(dhidden, dhidden_stride) || !lse || !workspace || ((uintptr_t)workspace & 255)) return TSLT_ERR_INVALID_ARG;
     const CeSpace s = ce_space(workspace, rows, V, D, true);
     if (workspace_bytes < s.bytes) return TSLT_ERR_WORKSPACE;
-    GatherParams g = {(const uint16_t*)hidden, target, hidden_stride, rows, V, D, lse, dloss, nullptr, nullptr, (uint16_t*)dhidden, dhidden_stride, s};
+    const GatherParams g = {(const uint16_t*)hidden, (const uint16_t*)weight, target, hidden_stride, weight_stride, rows, V, D, 0, lse, dloss,
+                            nullptr, nullptr, (uint16_t*)dhidden, dhidden_stride, s};
     if (const int rc = gather(g, st)) return rc;
     const uint16_t* w = (const uint16_t*)weight;
     const int tile_rows = s.pair ? 256 : 128, nt = D > 128 ? 256 : 128;
@@ -514,8 +595,8 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         gemm::Product p;
         CUtensorMap ta, tb;
         if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width, &p, &ta, &tb)) return rc;
-        const GradEpilogue::Params eg = {s.g, s.lse2, s.weight, s.target, s.piece, (int)v0, (int)width};
-        if (const int rc = product<GradEpilogue>(s.pair, ta, tb, p, eg, st)) return rc;
+        const GradEpilogue::Params eg = {s.g, s.lse2, s.weight, s.target, s.rows_pad, (int)v0, (int)width};
+        if (const int rc = product<GradEpilogue, 8>(s.pair, ta, tb, p, eg, st)) return rc;
 
         // dW of the piece: rows are vocabulary entries, the sum runs over the rows that count
         p.m_tiles = (int)(up(width, tile_rows) / tile_rows);
@@ -523,30 +604,36 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         p.nt = nt;
         p.k_blocks = (int)(s.rows_pad / 64);
         p.group_m = 8;
-        p.a_mn = p.b_mn = 1;
+        p.a_layout = p.b_layout = gemm::kBlocksMN;
         p.m_total = (int)width;
         p.m_limit = nullptr;
         p.k_limit = s.count;
-        if (!gemm::encode_map(&ta, false, s.g, s.piece, s.rows_pad, s.piece * 2, 64) ||
-            !gemm::encode_map(&tb, false, s.hidden, D, s.rows_pad, s.ds * 2, 64))
+        const int ctas = s.pair ? 2 : 1, b_blocks = nt / ctas / 64;
+        if (!gemm::encode_blocks(&ta, s.g, s.rows_pad, 128, s.piece / 64, s.rows_pad * 128, 2) ||
+            !gemm::encode_blocks(&tb, s.hidden, s.rows_pad, 128, s.ds / 64, s.rows_pad * 128, b_blocks))
             return TSLT_ERR_CUDA;
-        const WeightEpilogue::Params ew = {(uint16_t*)dweight + v0 * dweight_stride, dweight_stride, (int)width, D};
-        if (const int rc = product<WeightEpilogue>(s.pair, ta, tb, p, ew, st)) return rc;
+        uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
+        const int wide = ((uintptr_t)dw & 31) == 0 && dweight_stride % 16 == 0;
+        const WeightEpilogue::Params ew = {dw, s.top_weight, dweight_stride, (int)width, D, wide};
+        if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
 
         // the piece's part of dH: the sum runs over its vocabulary entries
         p.m_tiles = (int)(up(rows, tile_rows) / tile_rows);
         p.k_blocks = (int)((width + 63) / 64);
         p.splits = s.splits;
-        p.a_mn = 0;
+        p.a_layout = gemm::kPanelsK;
         p.m_total = rows;
         p.m_limit = s.count;
         p.k_limit = nullptr;
-        if (!gemm::encode_map(&ta, false, s.g, s.piece, s.rows_pad, s.piece * 2, 128) ||
-            !gemm::encode_map(&tb, false, w + v0 * weight_stride, D, width, weight_stride * 2, 64))
+        const uint16_t* wp = w + v0 * weight_stride;
+        p.b_layout = D % 64 == 0 ? gemm::kBlocksMN : gemm::kRowsMN;
+        if (!gemm::encode_map(&ta, false, s.g, 64, s.piece / 64 * s.rows_pad, 128, 128) ||
+            !(D % 64 == 0 ? gemm::encode_blocks(&tb, wp, width, weight_stride * 2, D / 64, 128, b_blocks)
+                          : gemm::encode_map(&tb, false, wp, D, width, weight_stride * 2, 64)))
             return TSLT_ERR_CUDA;
-        const HiddenEpilogue::Params eh = {s.acc, s.rows_pad, s.da, D, c == 0};
-        if (const int rc = product<HiddenEpilogue>(s.pair, ta, tb, p, eh, st)) return rc;
+        const HiddenEpilogue::Params eh = {(float4*)s.acc, s.rows_pad, s.da, D, c == 0};
+        if (const int rc = product<HiddenEpilogue, 4>(s.pair, ta, tb, p, eh, st)) return rc;
     }
-    ce_scatter_kernel<<<rows < 148 * 8 ? rows : 148 * 8, 256, 0, st>>>(s, (uint16_t*)dhidden, dhidden_stride, D);
+    ce_scatter_kernel<<<dim3((rows + 31) / 32, (D + 63) / 64), 256, 0, st>>>(s, (uint16_t*)dhidden, dhidden_stride, D);
     return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
 }
