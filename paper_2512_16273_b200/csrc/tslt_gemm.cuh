@@ -32,6 +32,8 @@ constexpr int kBarrierBytes = 1024;      // barriers and flags at the start of s
 constexpr int kStageA = 128 * 128;       // bytes of A per CTA and stage
 constexpr int kMaxStages = 12;
 constexpr int kSmemLimit = 227 * 1024;
+constexpr int kStageOut = 4096;          // bytes of an epilogue warp's output box: 32 rows of 128 bytes
+constexpr int kScratch = 256;            // bytes of an epilogue warp's scratch (where the epilogue has output boxes)
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 256;            // columns of one accumulator buffer
 constexpr int kWaitLimit = 1 << 22;
@@ -51,6 +53,10 @@ struct Product {
     uint32_t idesc;
     int clear_status;  // CTA 0 clears the status word first (another sets it only after a wait of kWaitLimit polls)
     int* status;
+};
+
+struct WarpSmem {  // an epilogue warp's own shared memory
+    uint32_t box, scratch;
 };
 
 struct Tile {
@@ -210,6 +216,17 @@ __device__ __forceinline__ uint32_t tmem_ld1(uint32_t addr) {  // one column, wa
     return v;
 }
 
+// An epilogue warp's output box: 32 rows of 64 bf16 columns, written with the 128-byte swizzle (16-byte chunk i of row r at
+// chunk i ^ (r mod 8)) and sent off by one lane as one copy, which clips it at the matrix's edges.
+__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t box, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(box) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int kPending> __device__ __forceinline__ void store_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kPending) : "memory");
+}
+__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, 8-row groups 1024 bytes apart (sbo).
 // MN-major: 64 contiguous elements of m per 128-byte row, one row per k; 8-k groups 1024 bytes apart (sbo), the next
 // 64 elements of m `lbo` bytes on.
@@ -292,7 +309,6 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
         }
         mbar_init(drain, 1);
         *abort_flag = 0;
-        if (p.clear_status && blockIdx.x == 0) *p.status = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&ta) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tb) : "memory");
@@ -303,6 +319,9 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
     else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(basep + 16 * kMaxStages + 40);
+    wait_for_primary_kernel();  // the set-up above overlaps the end of the kernel before this one in the call
+    allow_dependent_launch();
+    if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
     const Waiter wait = {abort_flag, p.status};
     const Walk walk(p, kTileRows);
 
@@ -387,6 +406,8 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
         }
     } else {
         const int quad = warp & 3, part = (warp - 2) >> 2;
+        const uint32_t out = data + p.stages * stage_bytes;
+        const WarpSmem own = {out + (warp - 2) * kStageOut, out + kEpiWarps * kStageOut + (warp - 2) * kScratch};
         int acc = 0, acc_phase = 0;
         for (int idx = cluster; idx < walk.total; idx += clusters) {
             const Tile t = walk.at(p, idx, kTileRows, rank);
@@ -397,7 +418,7 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
                 tc_fence_after();
             }
             Epi::template run<kEpiWarps / 4>(ep, tmem + ((uint32_t)(quad * 32) << 16) + acc * kAccCols, empty_sum, t, t.row0 + quad * 32 + lane,
-                                             lane, part);
+                                             lane, part, own);
             if (!empty_sum) {
                 tc_fence_before();
                 __syncwarp();
@@ -407,6 +428,7 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
             }
         }
     }
+    if (Epi::kOutBox && warp >= 2 && lane == 0) store_wait_all();
     __syncwarp();
     tc_fence_before();
     if (kCtas == 2) cluster_sync();
@@ -421,8 +443,9 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
 // A 2-d tensor map of `outer` rows of `inner` elements (row stride in bytes, a multiple of 16), boxes of box_inner x
 // box_outer with box_inner elements = 128 bytes.
 // encode_blocks: bf16 as [blocks][rows][64] (kBlocksMN), boxes of box_blocks x 64 x 64; strides in bytes.
+enum Element { kElemInt8, kElemBf16, kElemFp32 };
 bool encode_blocks(CUtensorMap* map, const void* base, long long rows, long long row_bytes, long long blocks, long long block_bytes, int box_blocks);
-bool encode_map(CUtensorMap* map, bool int8, const void* base, long long inner, long long outer, long long row_bytes, int box_outer);
+bool encode_map(CUtensorMap* map, Element e, const void* base, long long inner, long long outer, long long row_bytes, int box_outer);
 
 inline int sm_count() {  // of the current device; 0 if it cannot be found out
     static int cached[64] = {};
@@ -440,17 +463,18 @@ inline uint32_t instruction_desc(bool int8, int m, int n, bool a_mn, bool b_mn) 
     return d << 4 | ab << 7 | ab << 10 | (a_mn ? 1u << 15 : 0) | (b_mn ? 1u << 16 : 0) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
-// Fills idesc and stages from nt, launches on min(tiles, SMs) clusters.
+// Fills idesc and stages from nt, launches on min(tiles, SMs) clusters.  dependent: the kernel before it on the stream is
+// this call's own and its results are waited for inside (programmatic launch).
 template <bool kInt8, int kCtas, int kEpiWarps, class Epi>
-int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typename Epi::Params& ep, cudaStream_t st) {
+int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typename Epi::Params& ep, bool dependent, cudaStream_t st) {
     const int sms = sm_count();
     if (sms <= 0) return TSLT_ERR_CUDA;
-    const int stage = kStageA + p.nt / kCtas * 128;
-    p.stages = (kSmemLimit - 1024 - kBarrierBytes) / stage;
+    const int stage = kStageA + p.nt / kCtas * 128, boxes = Epi::kOutBox ? kEpiWarps * (kStageOut + kScratch) : 0;
+    p.stages = (kSmemLimit - 1024 - kBarrierBytes - boxes) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.idesc = instruction_desc(kInt8, 128 * kCtas, p.nt, p.a_layout >= kBlocksMN, p.b_layout >= kBlocksMN);
     auto kern = gemm_kernel<kInt8, kCtas, kEpiWarps, Epi>;
-    const int smem = 1024 + kBarrierBytes + p.stages * stage;
+    const int smem = 1024 + kBarrierBytes + p.stages * stage + boxes;
     static bool done[64] = {};
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return TSLT_ERR_CUDA;
@@ -467,14 +491,33 @@ int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typena
     cfg.blockDim = dim3(64 + 32 * kEpiWarps, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCtas;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = dependent;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCtas;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = kCtas > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, ta, tb, p, ep) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+}
+
+// The column width of a tile, a multiple of `unit`, at most 256: the one whose rounds of tiles over the machine's clusters cost
+// least, the widest of equals.  A stage costs nt + 256 (pair; nt + 128 for a single CTA) in units of its time in shared
+// memory, which its copies in and the tensor cores' reads share: 128 rows of A and the CTA's part of B, once each.
+inline int choose_nt(long long m_tiles, long long cols, bool pair, int unit) {
+    const long long slots = pair ? 74 : 148;
+    int best = 256;
+    long long least = -1;
+    for (int nt = 256; nt >= 64; nt -= unit) {
+        const long long tiles = m_tiles * ((cols + nt - 1) / nt), cost = (tiles + slots - 1) / slots * (nt + (pair ? 256 : 128));
+        if (least < 0 || cost < least) {
+            least = cost;
+            best = nt;
+        }
+    }
+    return best;
 }
 
 }  // namespace gemm

@@ -1,14 +1,18 @@
-// The head product in 8-bit integers (tslt_head_logits): z[n, v] = s_n t_v sum_k q[n, k] c[v, k].
+// The head product in 8-bit integers (tslt_head_logits): z[n, v] = s_n t_v sum_k q[n, k] c[v, k].  The sum is exact (32-bit
+// integers); the scales are multiplied in fp32 and the logit is rounded once.
 //
-// The weight is the operand of the tensor cores' 128 rows and the tokens are its columns: a decoding step has few tokens
-// (16 ... 256 columns), so the whole weight goes once through shared memory whatever their number, and a warp's lanes hold
-// consecutive vocabulary entries of one token, which is how the logits lie in memory.  The sum is exact (32-bit integers);
-// the scales are multiplied in fp32 and the logit is rounded once.
+// Few rows (a decoding step): bound by reading the weight once.  The weight is the operand of the tensor cores' 128 rows and
+// the tokens are its columns (16 ... 128), so that the whole weight goes once through shared memory whatever their number.
+//
+// Many rows (verification, prompts): bound by the tensor cores.  The tokens are the rows, 256 of them to a pair of CTAs, and a
+// lane of the epilogue holds 64 consecutive logits of a token, which leave through shared memory as whole 128-byte lines.
 #include "tslt_gemm.cuh"
 
 namespace tslt {
 
+// Few rows: lanes are vocabulary entries, columns are tokens.
 template <typename T> struct HeadEpilogue {
+    static constexpr bool kOutBox = false;
     struct Params {
         T* out;
         long long stride;
@@ -22,7 +26,7 @@ template <typename T> struct HeadEpilogue {
         *p = b;
     }
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int lane, int part) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int lane, int part, gemm::WarpSmem) {
         const bool on = v < p.V;
         const float wv = on ? __ldg(p.weight_scale + v) : 0.f;
         const int n = min(t.nt, p.rows - t.col0);
@@ -42,29 +46,113 @@ template <typename T> struct HeadEpilogue {
     }
 };
 
+// Many rows: lanes are tokens, columns are vocabulary entries.
+template <typename T> struct HeadRowsEpilogue {
+    static constexpr bool kOutBox = true;
+    static constexpr int kCols = 128 / sizeof(T);  // logits of a 128-byte line
+    struct Params {
+        CUtensorMap out;  // the logits' columns up to a multiple of 16 bytes (a copy writes 16 bytes or none)
+        T* rows;          // the same; the columns behind are stored one by one
+        long long stride;
+        const float *row_scale, *weight_scale;
+        int n_rows, V;
+    };
+    template <int kParts>
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part,
+                                               gemm::WarpSmem own) {
+        const float scale = row < p.n_rows ? __ldg(p.row_scale + row) : 0.f;
+        const uint32_t line = own.box + lane * 128;
+        constexpr int kStep = 16 / sizeof(T);
+        const int whole = p.V / kStep * kStep;
+        for (int c = part * kCols; c < t.nt && t.col0 + c < p.V; c += kParts * kCols) {
+            const int v0 = t.col0 + c;
+            // the columns' scales, a copy for each warp: 64 shuffles or loads would cost more than 16 reads of shared memory
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kCols; i += 32) {
+                const float w = v0 + i + lane < p.V ? __ldg(p.weight_scale + v0 + i + lane) : 0.f;
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(own.scratch + 4 * (i + lane)), "f"(w) : "memory");
+            }
+            __syncwarp();
+            uint32_t b[32];
+#pragma unroll
+            for (int i = 0; i < kCols; i += 32) {
+                uint32_t r[32];
+                gemm::tmem_ld32(tmem + c + i, r);
+                gemm::tmem_wait32(r);
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    float w[4], z[4];
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]) : "r"(own.scratch + 4 * (i + j)));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) z[k] = (float)(int)r[j + k] * scale * w[k];  // left to right, as the few-rows form
+                    if (sizeof(T) == 4) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) b[(j + k) & 31] = __float_as_uint(z[k]);
+                    } else {
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[((i + j) / 2) & 31]) : "f"(z[1]), "f"(z[0]));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[((i + j) / 2 + 1) & 31]) : "f"(z[3]), "f"(z[2]));
+                    }
+                }
+            }
+            if (lane == 0) gemm::store_wait_read<0>();  // the box's last copy has read it
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
+                             "r"(b[4 * i + 2]), "r"(b[4 * i + 3])
+                             : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && row < p.n_rows && v0 < whole) gemm::store_box(&p.out, own.box, v0, row);
+            if (whole < p.V && v0 + kCols > whole && row < p.n_rows) {
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) {
+                    if (v0 + j >= whole && v0 + j < p.V) {
+                        if (sizeof(T) == 4) reinterpret_cast<uint32_t*>(p.rows)[row * p.stride + v0 + j] = b[j & 31];
+                        else reinterpret_cast<uint16_t*>(p.rows)[row * p.stride + v0 + j] = (uint16_t)(b[(j / 2) & 31] >> (16 * (j & 1)));
+                    }
+                }
+            }
+        }
+    }
+};
+
+// Rows from which the tokens become the tensor cores' rows.
+constexpr int kManyRows = 129;
+
 template <typename T>
 static int launch_head(const signed char* q, const float* qs, long long q_stride, const signed char* w, const float* ws, long long w_stride,
                        int rows, int V, int K, T* out, long long out_stride, int* status, cudaStream_t st) {
     gemm::Product p = {};
-    const bool pair = rows > 64;
-    const int unit = 32;
-    p.n_tiles = (rows + 255) / 256;
-    p.nt = ((rows + p.n_tiles - 1) / p.n_tiles + unit - 1) / unit * unit;
-    if (rows <= 16) p.nt = 16;
-    const int tile_rows = pair ? 256 : 128;
-    p.m_tiles = (V + tile_rows - 1) / tile_rows;
     p.splits = 1;
     p.k_elems = 128;
     p.k_blocks = (K + 127) / 128;
-    p.group_m = 1;
-    p.m_total = V;
     p.status = status;
     p.clear_status = 1;
     CUtensorMap ta, tb;
-    if (!gemm::encode_map(&ta, true, w, K, V, w_stride, 128) || !gemm::encode_map(&tb, true, q, K, rows, q_stride, pair ? p.nt / 2 : p.nt))
-        return TSLT_ERR_CUDA;
+    if (rows >= kManyRows) {
+        p.m_tiles = (rows + 255) / 256;
+        p.nt = gemm::choose_nt(p.m_tiles, V, true, HeadRowsEpilogue<T>::kCols);
+        p.n_tiles = (V + p.nt - 1) / p.nt;
+        p.group_m = 16;
+        p.m_total = rows;
+        typename HeadRowsEpilogue<T>::Params ep = {{}, out, out_stride, qs, ws, rows, V};
+        const int step = 16 / sizeof(T);
+        if (!gemm::encode_map(&ta, gemm::kElemInt8, q, K, rows, q_stride, 128) || !gemm::encode_map(&tb, gemm::kElemInt8, w, K, V, w_stride, p.nt / 2) ||
+            !gemm::encode_map(&ep.out, sizeof(T) == 4 ? gemm::kElemFp32 : gemm::kElemBf16, out, V < step ? step : V / step * step, rows,
+                              out_stride * (long long)sizeof(T), 32))
+            return TSLT_ERR_CUDA;
+        return gemm::launch<true, 2, 8, HeadRowsEpilogue<T>>(ta, tb, p, ep, false, st);
+    }
+    p.nt = rows <= 16 ? 16 : (rows + 31) / 32 * 32;
+    p.n_tiles = 1;
+    p.m_tiles = (V + 127) / 128;
+    p.group_m = 1;
+    p.m_total = V;
+    if (!gemm::encode_map(&ta, gemm::kElemInt8, w, K, V, w_stride, 128) || !gemm::encode_map(&tb, gemm::kElemInt8, q, K, rows, q_stride, p.nt)) return TSLT_ERR_CUDA;
     const typename HeadEpilogue<T>::Params ep = {out, out_stride, qs, ws, rows, V};
-    return pair ? gemm::launch<true, 2, 8, HeadEpilogue<T>>(ta, tb, p, ep, st) : gemm::launch<true, 1, 8, HeadEpilogue<T>>(ta, tb, p, ep, st);
+    return gemm::launch<true, 1, 8, HeadEpilogue<T>>(ta, tb, p, ep, false, st);
 }
 
 }  // namespace tslt

@@ -42,7 +42,7 @@ struct CeSpace {
     uint16_t* g;       // panels [piece / 64][rows_pad][64]               (backward)
     float* acc;        // [splits][da / 4][rows_pad][4]                   (backward)
     long long rows_pad, ds, da, tiles, piece;
-    int pieces, splits, pair;
+    int pieces, splits, pair, nt;  // nt: columns of a tile of z (forward)
     size_t bytes;
 };
 
@@ -53,7 +53,8 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     s.da = up(D, 4);
     s.pair = rows > 128;
     const long long vt = up(V, kTileN);
-    s.tiles = vt / kTileN;
+    s.nt = gemm::choose_nt((rows + (s.pair ? 255 : 127)) / (s.pair ? 256 : 128), V, s.pair != 0, 32);
+    s.tiles = (V + s.nt - 1) / s.nt;
     long long c = kPieceBytes / 2 / s.rows_pad / kTileN * kTileN;
     if (c < kTileN) c = kTileN;
     s.pieces = (int)((vt + c - 1) / c);
@@ -144,6 +145,7 @@ __device__ __forceinline__ uint4 row_vec(const uint16_t* row, int i, int D) {
 __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_constant__ GatherParams p) {
     __shared__ int s_before, s_all;
     __shared__ uint32_t s_top;
+    allow_dependent_launch();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int first = min(p.rows, (int)blockIdx.x * p.per), last = min(p.rows, first + p.per);
     if (tid == 0) {
@@ -190,11 +192,20 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
                 const uint16_t *h = p.hidden + row * p.h_stride, *w = p.weight + t * p.w_stride;
                 uint4* dst = reinterpret_cast<uint4*>(p.s.hidden) + (size_t)at * 8;
                 float z = 0.f;
-#pragma unroll 4
-                for (int i = lane; i < vecs; i += 32) {
-                    const uint4 v = row_vec(h, i, p.D);
-                    if (p.loss) z = dot8(v, row_vec(w, i, p.D), z);
-                    dst[(size_t)(i >> 3) * p.s.rows_pad * 8 + (i & 7)] = v;
+                for (int i0 = lane; i0 < vecs; i0 += 128) {  // four (eight with the weight's row) loads in flight
+                    uint4 v[4], u[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = row_vec(h, i0 + 32 * k, p.D);
+                    if (p.loss) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) u[k] = row_vec(w, i0 + 32 * k, p.D);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int i = i0 + 32 * k;
+                        if (p.loss) z = dot8(v[k], u[k], z);
+                        if (i < vecs) dst[(size_t)(i >> 3) * p.s.rows_pad * 8 + (i & 7)] = v[k];
+                    }
                 }
                 if (p.loss) z = warp_sum(z);
                 if (lane == 0) {
@@ -240,6 +251,7 @@ __device__ __forceinline__ float pick_column(uint32_t tmem, int col, int lane) {
 }
 
 struct StatsEpilogue {
+    static constexpr bool kOutBox = false;
     struct Params {
         float2* part;
         const float* ztarget;
@@ -248,7 +260,7 @@ struct StatsEpilogue {
         int V;
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem) {
         const int n = min(t.nt, p.V - t.col0);
         float m = -INFINITY, s = 0.f;
         for (int c = part * 32; c < n; c += kParts * 32) {
@@ -284,7 +296,8 @@ struct StatsEpilogue {
     }
 };
 
-struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a tile that do not exist
+struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and the columns of a step of 64, that do not exist
+    static constexpr bool kOutBox = false;
     struct Params {
         uint16_t* g;
         const float *lse2, *weight;
@@ -293,13 +306,14 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
         int v0, n_real;  // first vocabulary entry of the piece; its entries
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem) {
         const bool on = row < t.rows;
         const float lse2 = on ? __ldg(p.lse2 + row) : 0.f, w = on ? __ldg(p.weight + row) : 0.f;
         const int col = on ? __ldg(p.target + row) - p.v0 - t.col0 : -1;
-        const int n = min(t.nt, p.n_real - t.col0);
+        const int n = min(t.nt, p.n_real - t.col0);  // its last columns, up to a multiple of 64, are zeros
         auto at = [&](int c) { return p.g + ((long long)((t.col0 + c) >> 6) * p.rows_pad + row) * 64 + ((t.col0 + c) & 63); };
-        for (int c = part * 32; c < t.nt; c += kParts * 32) {
+        const int end = min(t.nt, (p.n_real + 63) / 64 * 64 - t.col0);
+        for (int c = part * 32; c < end; c += kParts * 32) {
             uint32_t r[32];
             gemm::tmem_ld32(tmem + c, r);
             gemm::tmem_wait32(r);
@@ -327,61 +341,65 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows and columns of a
     }
 };
 
-struct WeightEpilogue {  // dW of a piece: rows are vocabulary entries
+// dW of a piece: rows are vocabulary entries.  A warp turns 32 rows x 64 columns at a time through its box of shared memory,
+// so that whole 128-byte lines go out (a lane's own 16-byte pieces, 2 KB apart, cost 37 instead of 20 us for 32001 x 1000).
+struct WeightEpilogue {
+    static constexpr bool kOutBox = true;
     struct Params {
-        uint16_t* out;  // of the piece's first entry
-        const float* scale;
+        CUtensorMap out;  // of the piece: its columns up to a multiple of 8 (a copy writes 16 bytes or none)
+        uint16_t* rows;   // the same; the columns behind are stored one by one
         long long stride;
-        int n_real, D, wide;  // wide: rows start on 32-byte boundaries
+        const float* scale;
+        int n_real, D;
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part) {
-        const bool on = row < p.n_real;
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int lane, int part,
+                                               gemm::WarpSmem own) {
         const float scale = __ldg(p.scale);
-        uint16_t* out = p.out + row * p.stride;
-        for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
-            uint32_t r[32];
-            gemm::tmem_ld32(tmem + c, r);
-            gemm::tmem_wait32(r);
-            uint32_t b[16];
+        const uint32_t line = own.box + lane * 128;
+        for (int c = part * 64; c < t.nt && t.col0 + c < p.D; c += kParts * 64) {
+            uint32_t r[32], b[32];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[j]) : "f"(__uint_as_float(r[2 * j + 1]) * scale), "f"(__uint_as_float(r[2 * j]) * scale));
-                if (zero) b[j] = 0;
-            }
-            const int d = t.col0 + c;
-            if (on) {
-                if (p.wide && d + 32 <= p.D) {  // whole sectors
+            for (int half = 0; half < 2; ++half) {
+                gemm::tmem_ld32(tmem + c + 32 * half, r);
+                gemm::tmem_wait32(r);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + d + 16 * j), "r"(b[8 * j]), "r"(b[8 * j + 1]),
-                                     "r"(b[8 * j + 2]), "r"(b[8 * j + 3]), "r"(b[8 * j + 4]), "r"(b[8 * j + 5]), "r"(b[8 * j + 6]), "r"(b[8 * j + 7])
-                                     : "memory");
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (d + 8 * j + 8 <= p.D) {
-                            *reinterpret_cast<uint4*>(out + d + 8 * j) = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                if (d + 8 * j + i < p.D) out[d + 8 * j + i] = (uint16_t)(b[4 * j + i / 2] >> (16 * (i & 1)));
-                        }
-                    }
+                for (int j = 0; j < 16; ++j) {
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;"
+                        : "=r"(b[16 * half + j])
+                        : "f"(__uint_as_float(r[2 * j + 1]) * scale), "f"(__uint_as_float(r[2 * j]) * scale));
+                    if (zero) b[16 * half + j] = 0;
                 }
+            }
+            if (lane == 0) gemm::store_wait_read<0>();  // the box's last copy has read it
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
+                             "r"(b[4 * i + 2]), "r"(b[4 * i + 3])
+                             : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            const int d = t.col0 + c, whole = p.D & ~7;
+            if (lane == 0 && row < p.n_real && d < whole) gemm::store_box(&p.out, own.box, d, row);
+            if (whole < p.D && d + 64 > whole && row < p.n_real) {
+#pragma unroll
+                for (int j = 0; j < 64; ++j)
+                    if (d + j >= whole && d + j < p.D) p.rows[row * p.stride + d + j] = (uint16_t)(b[j / 2] >> (16 * (j & 1)));
             }
         }
     }
 };
 
 struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer per cut of the sum), laid out so that a warp's rows are adjacent
+    static constexpr bool kOutBox = false;
     struct Params {
         float4* acc;
         long long rows_pad, da;
         int D, first;
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part, gemm::WarpSmem) {
         const bool on = row < t.rows;
         for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
             uint32_t r[32];
@@ -414,9 +432,10 @@ struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer p
 // ---- small kernels -----------------------------------------------------------------------------------------
 // Joins the tiles' (max, sum) pairs: a CTA takes 32 rows, its warps the tiles in turn; fp64 sums, a fixed order.
 constexpr int kJoinWarps = 32;
-__global__ void __launch_bounds__(32 * kJoinWarps) ce_join_kernel(CeSpace s, int parts, float* __restrict__ loss, float* __restrict__ lse) {
+__global__ void __launch_bounds__(32 * kJoinWarps) ce_join_kernel(CeSpace s, int parts, float* loss, float* lse) {
     __shared__ float s_m[kJoinWarps][32];
     __shared__ double s_s[kJoinWarps][32];
+    wait_for_primary_kernel();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x * 32 + lane, rows = *s.count;
     if ((int)blockIdx.x * 32 >= rows) return;
@@ -448,8 +467,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) ce_join_kernel(CeSpace s, int
 
 // dH: adds the cuts of the sum in order and puts the rows back in their places, times the largest weight.  A CTA takes 32 rows
 // by 64 hidden units: read as they lie (rows adjacent), turned in shared memory, written as 128-byte pieces of rows.
-__global__ void __launch_bounds__(256) ce_scatter_kernel(CeSpace s, uint16_t* __restrict__ out, long long stride, int D) {
+__global__ void __launch_bounds__(256) ce_scatter_kernel(CeSpace s, uint16_t* out, long long stride, int D) {
     __shared__ uint32_t tile[32][33];
+    wait_for_primary_kernel();
     const int rows = *s.count, r0 = blockIdx.x * 32, d0 = blockIdx.y * 64;
     if (r0 >= rows) return;
     const float scale = *s.top_weight;
@@ -461,6 +481,7 @@ __global__ void __launch_bounds__(256) ce_scatter_kernel(CeSpace s, uint16_t* __
         if (d < D && r0 + lane < rows) {
             const float4* a = acc + (long long)(d / 4) * s.rows_pad + r0 + lane;
             float4 v = *a;
+#pragma unroll 8
             for (int i = 1; i < s.splits; ++i) {
                 const float4 w = a[i * (s.da / 4) * s.rows_pad];
                 v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
@@ -490,19 +511,33 @@ static int gather(GatherParams p, cudaStream_t st) {
     return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
 }
 
+template <typename... Args>
+static int launch_after(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+}
+
 template <class Epi, int kWarps>
 static int product(bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const gemm::Product& p, const typename Epi::Params& ep, cudaStream_t st) {
-    return pair ? gemm::launch<false, 2, kWarps, Epi>(ta, tb, p, ep, st) : gemm::launch<false, 1, kWarps, Epi>(ta, tb, p, ep, st);
+    return pair ? gemm::launch<false, 2, kWarps, Epi>(ta, tb, p, ep, true, st) : gemm::launch<false, 1, kWarps, Epi>(ta, tb, p, ep, true, st);
 }
 
 // z of `width` vocabulary entries from row v0 of the weight: the product that forward and backward share.
-static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, long long w_stride, long long width, gemm::Product* p,
+static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, long long w_stride, long long width, int nt, gemm::Product* p,
                           CUtensorMap* ta, CUtensorMap* tb) {
     *p = gemm::Product{};
     const int tile_rows = s.pair ? 256 : 128;
     p->m_tiles = (int)(up(rows, tile_rows) / tile_rows);
-    p->nt = kTileN;
-    p->n_tiles = (int)(up(width, kTileN) / kTileN);
+    p->nt = nt;
+    p->n_tiles = (int)((width + nt - 1) / nt);
     p->splits = 1;
     p->k_elems = 64;
     p->k_blocks = (D + 63) / 64;
@@ -512,8 +547,8 @@ static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, 
     p->status = s.status;
     p->a_layout = gemm::kPanelsK;
     p->pitch = (int)s.rows_pad;
-    return gemm::encode_map(ta, false, s.hidden, 64, s.ds / 64 * s.rows_pad, 128, 128) &&
-                   gemm::encode_map(tb, false, w, D, width, w_stride * 2, s.pair ? kTileN / 2 : kTileN)
+    return gemm::encode_map(ta, gemm::kElemBf16, s.hidden, 64, s.ds / 64 * s.rows_pad, 128, 128) &&
+                   gemm::encode_map(tb, gemm::kElemBf16, w, D, width, w_stride * 2, s.pair ? nt / 2 : nt)
                ? TSLT_OK
                : TSLT_ERR_CUDA;
 }
@@ -561,14 +596,13 @@ extern "C" int tslt_linear_ce(const void* hidden, long long hidden_stride, const
     cudaStream_t st = (cudaStream_t)stream;
     gemm::Product p;
     CUtensorMap ta, tb;
-    if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, &p, &ta, &tb)) return rc;
+    if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, s.nt, &p, &ta, &tb)) return rc;
     const GatherParams g = {(const uint16_t*)hidden, (const uint16_t*)weight, target, hidden_stride, weight_stride, rows, V, D, 0, nullptr,
                             nullptr, loss, lse, nullptr, 0, s};
     if (const int rc = gather(g, st)) return rc;
     const StatsEpilogue::Params ep = {s.part, s.ztarget, s.target, s.rows_pad, V};
     if (const int rc = product<StatsEpilogue, 4 * kStatsParts>(s.pair, ta, tb, p, ep, st)) return rc;
-    ce_join_kernel<<<(rows + 31) / 32, 32 * kJoinWarps, 0, st>>>(s, (int)s.tiles * kStatsParts, loss, lse);
-    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    return launch_after(ce_join_kernel, dim3((rows + 31) / 32), 32 * kJoinWarps, st, s, (int)s.tiles * kStatsParts, loss, lse);
 }
 
 extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stride, const void* weight, long long weight_stride,
@@ -594,7 +628,8 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         const long long v0 = c * s.piece, width = v0 + s.piece < V ? s.piece : V - v0;
         gemm::Product p;
         CUtensorMap ta, tb;
-        if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width, &p, &ta, &tb)) return rc;
+        if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width,
+                                         gemm::choose_nt((rows + tile_rows - 1) / tile_rows, width, s.pair != 0, 32), &p, &ta, &tb)) return rc;
         const GradEpilogue::Params eg = {s.g, s.lse2, s.weight, s.target, s.rows_pad, (int)v0, (int)width};
         if (const int rc = product<GradEpilogue, 8>(s.pair, ta, tb, p, eg, st)) return rc;
 
@@ -613,9 +648,9 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
             !gemm::encode_blocks(&tb, s.hidden, s.rows_pad, 128, s.ds / 64, s.rows_pad * 128, b_blocks))
             return TSLT_ERR_CUDA;
         uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
-        const int wide = ((uintptr_t)dw & 31) == 0 && dweight_stride % 16 == 0;
-        const WeightEpilogue::Params ew = {dw, s.top_weight, dweight_stride, (int)width, D, wide};
-        if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
+        WeightEpilogue::Params ew = {{}, dw, dweight_stride, s.top_weight, (int)width, D};
+        if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
+        if (const int rc = product<WeightEpilogue, 8>(s.pair, ta, tb, p, ew, st)) return rc;
 
         // the piece's part of dH: the sum runs over its vocabulary entries
         p.m_tiles = (int)(up(rows, tile_rows) / tile_rows);
@@ -627,13 +662,12 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         p.k_limit = nullptr;
         const uint16_t* wp = w + v0 * weight_stride;
         p.b_layout = D % 64 == 0 ? gemm::kBlocksMN : gemm::kRowsMN;
-        if (!gemm::encode_map(&ta, false, s.g, 64, s.piece / 64 * s.rows_pad, 128, 128) ||
+        if (!gemm::encode_map(&ta, gemm::kElemBf16, s.g, 64, s.piece / 64 * s.rows_pad, 128, 128) ||
             !(D % 64 == 0 ? gemm::encode_blocks(&tb, wp, width, weight_stride * 2, D / 64, 128, b_blocks)
-                          : gemm::encode_map(&tb, false, wp, D, width, weight_stride * 2, 64)))
+                          : gemm::encode_map(&tb, gemm::kElemBf16, wp, D, width, weight_stride * 2, 64)))
             return TSLT_ERR_CUDA;
         const HiddenEpilogue::Params eh = {(float4*)s.acc, s.rows_pad, s.da, D, c == 0};
         if (const int rc = product<HiddenEpilogue, 4>(s.pair, ta, tb, p, eh, st)) return rc;
     }
-    ce_scatter_kernel<<<dim3((rows + 31) / 32, (D + 63) / 64), 256, 0, st>>>(s, (uint16_t*)dhidden, dhidden_stride, D);
-    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    return launch_after(ce_scatter_kernel, dim3((rows + 31) / 32, (D + 63) / 64), 256, st, s, (uint16_t*)dhidden, dhidden_stride, D);
 }

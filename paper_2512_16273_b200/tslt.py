@@ -746,8 +746,9 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _stream_on(dev: int) -> int:
-    return torch.cuda.current_stream(dev).cuda_stream
+# The current stream's handle without building a Stream object (1.3 us of a call), where torch has it.
+_stream_on = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _check_tensor(t, name: str, dtype, dev: int) -> None:
@@ -795,16 +796,54 @@ def _rows_like(lead, cols: int, dtype, device) -> torch.Tensor:
     """An empty [*lead, cols] whose rows start on 16-byte boundaries."""
     step = _STEP[dtype]
     if cols % step == 0:
-        return torch.empty(*lead, cols, dtype=dtype, device=device)
-    return torch.empty(*lead, -(-cols // step) * step, dtype=dtype, device=device)[..., :cols]
+        return torch.empty((*lead, cols), dtype=dtype, device=device)
+    strides = [1, -(-cols // step) * step]
+    for n in reversed(lead[1:]):
+        strides.append(strides[-1] * n)
+    return torch.empty_strided((*lead, cols), strides[::-1] if lead else (1,), dtype=dtype, device=device)
+
+
+def _like(x: torch.Tensor, dtype, cols: int) -> torch.Tensor:
+    """An empty tensor of x's shape [..., cols] whose rows start on 16-byte boundaries."""
+    if cols % 16 == 0 and x.is_contiguous():
+        return torch.empty_like(x, dtype=dtype)
+    return _rows_like(x.shape[:-1], cols, dtype, x.device)
+
+
+def _given(out: dict, name: str, shape, dtype, dev: int):
+    """out[name] checked, or None where `out` has none."""
+    t = out.get(name)
+    if t is None:
+        return None
+    _check_tensor(t, "output " + name, dtype, dev)
+    if t.shape != shape:
+        raise ValueError("output %s must have shape %s" % (name, tuple(shape)))
+    if len(shape) == 1 and not t.is_contiguous():
+        raise ValueError("output %s must be contiguous" % name)
+    return t
+
+
+def _stride(t: torch.Tensor, cols: int, name: str) -> int:
+    """Row stride of a matrix output [..., cols]."""
+    if t.dim() == 2 and t.shape[0] > 1 and t.stride(1) == 1 and t.stride(0) >= cols:
+        return t.stride(0)
+    return _matrix(t, "output " + name, None, t.get_device(), cols)[2]
+
+
+_head_ws: Dict[tuple, torch.Tensor] = {}
 
 
 def _scratch(nbytes: int, device) -> torch.Tensor:
-    """The stream's cached workspace; under graph capture a buffer of the graph's own, so that two captured graphs
-    never share one."""
+    """A workspace of the current stream's, kept for its next call; under graph capture a buffer of the graph's own, so
+    that two captured graphs never share one."""
     if torch.cuda.is_current_stream_capturing():
         return torch.empty(max(int(nbytes), 4096), dtype=torch.uint8, device=device)
-    return workspace(nbytes, device)
+    key = (device.index, _stream_on(device.index))
+    ws = _head_ws.get(key)
+    if ws is None or ws.numel() < nbytes:
+        ws = torch.empty(max(int(nbytes), 4096), dtype=torch.uint8, device=device)
+        _head_ws[key] = ws
+    return ws
 
 
 def _space(ws, nbytes: int, device, dev: int) -> torch.Tensor:
@@ -826,7 +865,7 @@ def rmsnorm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
     residual itself."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("x must be a CUDA tensor (libtslt has no CPU path)")
-    code, dev, device, shape = _dtype_code(x), x.get_device(), x.device, x.shape
+    code, dev, shape = _dtype_code(x), x.get_device(), x.shape
     rows, D, xs = _matrix(x, "x", None, dev)
     rs = hs = vs = 0
     if residual is not None:
@@ -835,25 +874,35 @@ def rmsnorm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
         rs = _matrix(residual, "residual", x.dtype, dev, D)[2]
     if weight is not None:
         _vector(weight, "weight", x.dtype, dev, D)
-    o = out if out is not None else {}
-    lead = shape[:-1]
-    if "q" not in o:
-        o["q"] = _rows_like(lead, D, torch.int8, device)
-    if "scale" not in o:
-        o["scale"] = torch.empty(rows, dtype=torch.float32, device=device)
-    if residual is not None and "residual" not in o:
-        o["residual"] = _rows_like(lead, D, x.dtype, device)
-    if want_values and "values" not in o:
-        o["values"] = _rows_like(lead, D, torch.bfloat16, device)
-    q, scale, h, y = o["q"], o["scale"], o.get("residual"), o.get("values")
-    if q.shape != shape or (h is not None and h.shape != shape) or (y is not None and y.shape != shape):
-        raise ValueError("outputs q, residual and values must have the shape of x")
-    qs = _matrix(q, "q", torch.int8, dev, D)[2]
-    if h is not None:
-        hs = _matrix(h, "output residual", x.dtype, dev, D)[2]
-    if y is not None:
-        vs = _matrix(y, "output values", torch.bfloat16, dev, D)[2]
-    _vector(scale, "scale", torch.float32, dev, rows)
+    if out is None and D % 16 == 0 and x.is_contiguous():  # the ordinary call: nothing to look at in the outputs
+        q, scale = torch.empty_like(x, dtype=torch.int8), x.new_empty(rows, dtype=torch.float32)
+        h = None if residual is None else torch.empty_like(x)
+        y = torch.empty_like(x, dtype=torch.bfloat16) if want_values else None
+        qs = hs = vs = D
+        o = {"q": q, "scale": scale}
+        if h is not None:
+            o["residual"] = h
+        if y is not None:
+            o["values"] = y
+    else:
+        o = {} if out is None else out
+        q, scale = _given(o, "q", shape, torch.int8, dev), _given(o, "scale", (rows,), torch.float32, dev)
+        h, y = _given(o, "residual", shape, x.dtype, dev), _given(o, "values", shape, torch.bfloat16, dev)
+        if h is not None and residual is None:
+            raise ValueError("output residual needs a residual")
+        if q is None:
+            q = o["q"] = _like(x, torch.int8, D)
+        if scale is None:
+            scale = o["scale"] = x.new_empty(rows, dtype=torch.float32)
+        if h is None and residual is not None:
+            h = o["residual"] = _like(x, x.dtype, D)
+        if y is None and want_values:
+            y = o["values"] = _like(x, torch.bfloat16, D)
+        qs = _stride(q, D, "q")
+        if h is not None:
+            hs = _stride(h, D, "residual")
+        if y is not None:
+            vs = _stride(y, D, "values")
     _check(lib().tslt_rmsnorm_quant(_at(x), _at(residual), _at(weight), code, rows, D, xs, rs, eps, _at(h), hs, _at(y), vs,
                                     _at(q), qs, _at(scale), _stream_on(dev)), "tslt_rmsnorm_quant")
     return o
@@ -867,15 +916,12 @@ def quantize_rows(x: torch.Tensor, *, out: Optional[dict] = None) -> dict:
         raise ValueError("x must be a CUDA tensor (libtslt has no CPU path)")
     code, dev, device = _dtype_code(x), x.get_device(), x.device
     rows, D, xs = _matrix(x, "x", None, dev)
-    o = out if out is not None else {}
-    if "q" not in o:
-        o["q"] = _rows_like(x.shape[:-1], D, torch.int8, device)
-    if "scale" not in o:
+    o = {} if out is None else out
+    if _given(o, "q", x.shape, torch.int8, dev) is None:
+        o["q"] = _like(x, torch.int8, D)
+    if _given(o, "scale", (rows,), torch.float32, dev) is None:
         o["scale"] = torch.empty(rows, dtype=torch.float32, device=device)
-    if o["q"].shape != x.shape:
-        raise ValueError("output q must have the shape of x")
-    qs = _matrix(o["q"], "q", torch.int8, dev, D)[2]
-    _vector(o["scale"], "scale", torch.float32, dev, rows)
+    qs = _stride(o["q"], D, "q")
     _check(lib().tslt_quantize_rows(_at(x), code, rows, D, xs, _at(o["q"]), qs, _at(o["scale"]), _stream_on(dev)),
            "tslt_quantize_rows")
     return o
@@ -899,13 +945,11 @@ def head_logits(q: torch.Tensor, scale: torch.Tensor, weight: torch.Tensor, weig
     _vector(weight_scale, "weight_scale", torch.float32, dev, V)
     if logits_dtype not in (torch.float32, torch.bfloat16):
         raise TsltError(ERR_UNSUPPORTED, "dtype %s" % logits_dtype)
-    o = out if out is not None else {}
-    if "logits" not in o:
-        o["logits"] = _rows_like(q.shape[:-1], V, logits_dtype, device)
-    z = o["logits"]
-    zr, _, zs = _matrix(z, "logits", logits_dtype, dev, V)
-    if zr != rows:
-        raise ValueError("output logits must have %d rows" % rows)
+    o = {} if out is None else out
+    z = _given(o, "logits", (*q.shape[:-1], V), logits_dtype, dev)
+    if z is None:
+        z = o["logits"] = _rows_like(q.shape[:-1], V, logits_dtype, device)
+    zs = _stride(z, V, "logits")
     ws = _space(ws, 256, device, dev)
     _check(lib().tslt_head_logits(_at(q), _at(scale), qs, _at(weight), _at(weight_scale), wstride, rows, V, D,
                                   F32 if logits_dtype == torch.float32 else BF16, _at(z), zs, _at(ws), ws.numel(), _stream_on(dev)),
@@ -967,11 +1011,10 @@ def linear_ce(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, 
     Returns dict(loss [rows], lse [rows] fp32, workspace), both 0 in ignored rows."""
     dev, rows, V, D, hs, wstride = _loss_inputs(hidden, weight, target)
     device = hidden.device
-    o = out if out is not None else {}
+    o = {} if out is None else out
     for name in ("loss", "lse"):
-        if name not in o:
+        if _given(o, name, (rows,), torch.float32, dev) is None:
             o[name] = torch.empty(rows, dtype=torch.float32, device=device)
-        _vector(o[name], name, torch.float32, dev, rows)
     ws = _space(ws, linear_ce_workspace_bytes(rows, V, D), device, dev)
     _check(lib().tslt_linear_ce(_at(hidden), hs, _at(weight), wstride, _at(target), rows, V, D, _at(o["loss"]),
                                 _at(o["lse"]), _at(ws), ws.numel(), _stream_on(dev)), "tslt_linear_ce")
@@ -991,15 +1034,11 @@ def linear_ce_backward(hidden: torch.Tensor, weight: torch.Tensor, target: torch
     _vector(lse, "lse", torch.float32, dev, rows)
     if dloss is not None:
         _vector(dloss, "dloss", torch.float32, dev, rows)
-    o = out if out is not None else {}
-    if "dhidden" not in o:
-        o["dhidden"] = _rows_like(hidden.shape[:-1], D, torch.bfloat16, device)
-    if "dweight" not in o:
-        o["dweight"] = _rows_like((V,), D, torch.bfloat16, device)
-    dr, _, dhs = _matrix(o["dhidden"], "dhidden", torch.bfloat16, dev, D)
-    dv, _, dws = _matrix(o["dweight"], "dweight", torch.bfloat16, dev, D)
-    if dr != rows or dv != V:
-        raise ValueError("output dhidden must have %d rows and dweight %d" % (rows, V))
+    o = {} if out is None else out
+    for name, t in (("dhidden", hidden), ("dweight", weight)):
+        if _given(o, name, t.shape, torch.bfloat16, dev) is None:
+            o[name] = _like(t, torch.bfloat16, D)
+    dhs, dws = _stride(o["dhidden"], D, "dhidden"), _stride(o["dweight"], D, "dweight")
     ws = _space(ws, linear_ce_backward_workspace_bytes(rows, V, D), device, dev)
     _check(lib().tslt_linear_ce_backward(_at(hidden), hs, _at(weight), wstride, _at(target), _at(lse), _at(dloss), rows, V, D,
                                          _at(o["dhidden"]), dhs, _at(o["dweight"]), dws, _at(ws), ws.numel(), _stream_on(dev)),
