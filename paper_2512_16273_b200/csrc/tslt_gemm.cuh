@@ -55,8 +55,14 @@ struct Product {
     int* status;
 };
 
-struct WarpSmem {  // an epilogue warp's own shared memory
+struct WarpSmem {  // an epilogue warp's own shared memory: kBoxes output boxes used in turn, and a scratch
     uint32_t box, scratch;
+    int turn;
+    __device__ __forceinline__ uint32_t next() {
+        const uint32_t b = box + turn * 4096;
+        turn ^= 1;
+        return b;
+    }
 };
 
 struct Tile {
@@ -407,7 +413,7 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
     } else {
         const int quad = warp & 3, part = (warp - 2) >> 2;
         const uint32_t out = data + p.stages * stage_bytes;
-        const WarpSmem own = {out + (warp - 2) * kStageOut, out + kEpiWarps * kStageOut + (warp - 2) * kScratch};
+        WarpSmem own = {out + (warp - 2) * 2 * kStageOut, out + kEpiWarps * 2 * kStageOut + (warp - 2) * kScratch, 0};
         int acc = 0, acc_phase = 0;
         for (int idx = cluster; idx < walk.total; idx += clusters) {
             const Tile t = walk.at(p, idx, kTileRows, rank);
@@ -469,7 +475,7 @@ template <bool kInt8, int kCtas, int kEpiWarps, class Epi>
 int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typename Epi::Params& ep, bool dependent, cudaStream_t st) {
     const int sms = sm_count();
     if (sms <= 0) return TSLT_ERR_CUDA;
-    const int stage = kStageA + p.nt / kCtas * 128, boxes = Epi::kOutBox ? kEpiWarps * (kStageOut + kScratch) : 0;
+    const int stage = kStageA + p.nt / kCtas * 128, boxes = Epi::kOutBox ? kEpiWarps * (2 * kStageOut + kScratch) : 0;
     p.stages = (kSmemLimit - 1024 - kBarrierBytes - boxes) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.idesc = instruction_desc(kInt8, 128 * kCtas, p.nt, p.a_layout >= kBlocksMN, p.b_layout >= kBlocksMN);

@@ -26,7 +26,7 @@ template <typename T> struct HeadEpilogue {
         *p = b;
     }
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int lane, int part, gemm::WarpSmem) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int lane, int part, gemm::WarpSmem&) {
         const bool on = v < p.V;
         const float wv = on ? __ldg(p.weight_scale + v) : 0.f;
         const int n = min(t.nt, p.rows - t.col0);
@@ -59,9 +59,8 @@ template <typename T> struct HeadRowsEpilogue {
     };
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part,
-                                               gemm::WarpSmem own) {
+                                               gemm::WarpSmem& own) {
         const float scale = row < p.n_rows ? __ldg(p.row_scale + row) : 0.f;
-        const uint32_t line = own.box + lane * 128;
         constexpr int kStep = 16 / sizeof(T);
         const int whole = p.V / kStep * kStep;
         for (int c = part * kCols; c < t.nt && t.col0 + c < p.V; c += kParts * kCols) {
@@ -95,8 +94,9 @@ template <typename T> struct HeadRowsEpilogue {
                     }
                 }
             }
-            if (lane == 0) gemm::store_wait_read<0>();  // the box's last copy has read it
+            if (lane == 0) gemm::store_wait_read<1>();  // the last copy but one, which was of this box, has read it
             __syncwarp();
+            const uint32_t box = own.next(), line = box + lane * 128;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
@@ -104,7 +104,7 @@ template <typename T> struct HeadRowsEpilogue {
                              : "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0 && row < p.n_rows && v0 < whole) gemm::store_box(&p.out, own.box, v0, row);
+            if (lane == 0 && row < p.n_rows && v0 < whole) gemm::store_box(&p.out, box, v0, row);
             if (whole < p.V && v0 + kCols > whole && row < p.n_rows) {
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) {
@@ -143,7 +143,7 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
             !gemm::encode_map(&ep.out, sizeof(T) == 4 ? gemm::kElemFp32 : gemm::kElemBf16, out, V < step ? step : V / step * step, rows,
                               out_stride * (long long)sizeof(T), 32))
             return TSLT_ERR_CUDA;
-        return gemm::launch<true, 2, 8, HeadRowsEpilogue<T>>(ta, tb, p, ep, false, st);
+        return gemm::launch<true, 2, 4, HeadRowsEpilogue<T>>(ta, tb, p, ep, false, st);
     }
     p.nt = rows <= 16 ? 16 : (rows + 31) / 32 * 32;
     p.n_tiles = 1;

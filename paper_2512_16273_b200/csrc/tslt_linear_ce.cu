@@ -61,8 +61,9 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     s.piece = up((vt + s.pieces - 1) / s.pieces, kTileN);
     s.pieces = (int)((vt + s.piece - 1) / s.piece);
     // dH: cut its sum over the piece so that the last round of tiles wastes little.  How many rows count is only known on
-    // the device: the rule averages over all of them and three quarters, and charges 1.5 % for each further buffer.  Few
-    // rows have few tiles and a long sum: there, as many cuts as fill the machine.
+    // the device: the rule averages over all of them and three quarters, and charges each buffer what adding to it costs
+    // next to a piece's products (3.4 % at 16128 entries, measured; it goes with 1 / piece).  Few rows have few tiles and
+    // a long sum: there, as many cuts as fill the machine.
     const long long tile_rows = s.pair ? 256 : 128, slots = s.pair ? 74 : 148, cols = up(D, kTileN) / kTileN;
     const long long m_all = up(rows, tile_rows) / tile_rows, m_less = up((rows * 3ll + 3) / 4, tile_rows) / tile_rows;
     auto waste = [&](long long tiles, long long cuts) { return (double)(up(tiles * cuts, slots)) / (double)(tiles * cuts); };
@@ -72,7 +73,7 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     s.splits = 1;
     double best = 1e30;
     for (long long c = 1; c <= most; ++c) {
-        const double cost = (waste(m_all * cols, c) + waste(m_less * cols, c)) * 0.5 + 0.015 * (double)c * (double)(m_all * cols) / slots;
+        const double cost = (waste(m_all * cols, c) + waste(m_less * cols, c)) * 0.5 + (s.pieces > 1 ? 550.0 : 275.0) / (double)s.piece * (double)c;
         if (cost < best) {
             best = cost;
             s.splits = (int)c;
@@ -260,7 +261,7 @@ struct StatsEpilogue {
         int V;
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem&) {
         const int n = min(t.nt, p.V - t.col0);
         float m = -INFINITY, s = 0.f;
         for (int c = part * 32; c < n; c += kParts * 32) {
@@ -306,7 +307,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and t
         int v0, n_real;  // first vocabulary entry of the piece; its entries
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem&) {
         const bool on = row < t.rows;
         const float lse2 = on ? __ldg(p.lse2 + row) : 0.f, w = on ? __ldg(p.weight + row) : 0.f;
         const int col = on ? __ldg(p.target + row) - p.v0 - t.col0 : -1;
@@ -354,9 +355,8 @@ struct WeightEpilogue {
     };
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int lane, int part,
-                                               gemm::WarpSmem own) {
+                                               gemm::WarpSmem& own) {
         const float scale = __ldg(p.scale);
-        const uint32_t line = own.box + lane * 128;
         for (int c = part * 64; c < t.nt && t.col0 + c < p.D; c += kParts * 64) {
             uint32_t r[32], b[32];
 #pragma unroll
@@ -371,8 +371,9 @@ struct WeightEpilogue {
                     if (zero) b[16 * half + j] = 0;
                 }
             }
-            if (lane == 0) gemm::store_wait_read<0>();  // the box's last copy has read it
+            if (lane == 0) gemm::store_wait_read<1>();  // the last copy but one, which was of this box, has read it
             __syncwarp();
+            const uint32_t box = own.next(), line = box + lane * 128;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
@@ -381,7 +382,7 @@ struct WeightEpilogue {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             const int d = t.col0 + c, whole = p.D & ~7;
-            if (lane == 0 && row < p.n_real && d < whole) gemm::store_box(&p.out, own.box, d, row);
+            if (lane == 0 && row < p.n_real && d < whole) gemm::store_box(&p.out, box, d, row);
             if (whole < p.D && d + 64 > whole && row < p.n_real) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
@@ -399,7 +400,7 @@ struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer p
         int D, first;
     };
     template <int kParts>
-    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part, gemm::WarpSmem) {
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part, gemm::WarpSmem&) {
         const bool on = row < t.rows;
         for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
             uint32_t r[32];
@@ -465,40 +466,57 @@ __global__ void __launch_bounds__(32 * kJoinWarps) ce_join_kernel(CeSpace s, int
     }
 }
 
-// dH: adds the cuts of the sum in order and puts the rows back in their places, times the largest weight.  A CTA takes 32 rows
-// by 64 hidden units: read as they lie (rows adjacent), turned in shared memory, written as 128-byte pieces of rows.
-__global__ void __launch_bounds__(256) ce_scatter_kernel(CeSpace s, uint16_t* out, long long stride, int D) {
+// dH: adds the cuts of the sum and puts the rows back in their places, times the largest weight.  A CTA takes 32 rows by 64
+// hidden units: read as they lie (rows adjacent), turned in shared memory, written as 128-byte pieces of rows.  With many
+// cuts (few rows) kGroups of warps share them, each adding its own in order.
+template <int kGroups>
+__global__ void __launch_bounds__(256 * kGroups) ce_scatter_kernel(CeSpace s, uint16_t* out, long long stride, int D) {
+    __shared__ float4 sums[kGroups > 1 ? kGroups - 1 : 1][16][32];
     __shared__ uint32_t tile[32][33];
     wait_for_primary_kernel();
     const int rows = *s.count, r0 = blockIdx.x * 32, d0 = blockIdx.y * 64;
     if (r0 >= rows) return;
     const float scale = *s.top_weight;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 7, group = threadIdx.x >> 8;
     const float4* acc = reinterpret_cast<const float4*>(s.acc);
+    const int from = s.splits * group / kGroups, to = s.splits * (group + 1) / kGroups;
+    float4 v[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int c4 = warp + 8 * k, d = d0 + 4 * c4;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (d < D && r0 + lane < rows) {
             const float4* a = acc + (long long)(d / 4) * s.rows_pad + r0 + lane;
-            float4 v = *a;
 #pragma unroll 8
-            for (int i = 1; i < s.splits; ++i) {
+            for (int i = from; i < to; ++i) {
                 const float4 w = a[i * (s.da / 4) * s.rows_pad];
-                v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+                v[k] = make_float4(v[k].x + w.x, v[k].y + w.y, v[k].z + w.z, v[k].w + w.w);
             }
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(tile[lane][2 * c4]) : "f"(v.y * scale), "f"(v.x * scale));
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(tile[lane][2 * c4 + 1]) : "f"(v.w * scale), "f"(v.z * scale));
+        }
+        if (group > 0) sums[group - 1][c4][lane] = v[k];
+    }
+    if (kGroups > 1) __syncthreads();
+    if (group == 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int c4 = warp + 8 * k;
+#pragma unroll
+            for (int g = 0; g + 1 < kGroups; ++g) {
+                const float4 w = sums[g][c4][lane];
+                v[k] = make_float4(v[k].x + w.x, v[k].y + w.y, v[k].z + w.z, v[k].w + w.w);
+            }
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(tile[lane][2 * c4]) : "f"(v[k].y * scale), "f"(v[k].x * scale));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(tile[lane][2 * c4 + 1]) : "f"(v[k].w * scale), "f"(v[k].z * scale));
         }
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int r = warp + 8 * k, d = d0 + 2 * lane;
+    for (int r = threadIdx.x >> 5; r < 32; r += 8 * kGroups) {
+        const int d = d0 + 2 * lane;
         if (r0 + r < rows && d < D) {
             uint16_t* o = out + s.row_of[r0 + r] * stride + d;
-            const uint32_t v = tile[r][lane];
-            if (d + 1 < D) *reinterpret_cast<uint32_t*>(o) = v;
-            else *o = (uint16_t)v;
+            const uint32_t w = tile[r][lane];
+            if (d + 1 < D) *reinterpret_cast<uint32_t*>(o) = w;
+            else *o = (uint16_t)w;
         }
     }
 }
@@ -650,7 +668,7 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
         WeightEpilogue::Params ew = {{}, dw, dweight_stride, s.top_weight, (int)width, D};
         if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
-        if (const int rc = product<WeightEpilogue, 8>(s.pair, ta, tb, p, ew, st)) return rc;
+        if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
 
         // the piece's part of dH: the sum runs over its vocabulary entries
         p.m_tiles = (int)(up(rows, tile_rows) / tile_rows);
@@ -669,5 +687,7 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         const HiddenEpilogue::Params eh = {(float4*)s.acc, s.rows_pad, s.da, D, c == 0};
         if (const int rc = product<HiddenEpilogue, 4>(s.pair, ta, tb, p, eh, st)) return rc;
     }
-    return launch_after(ce_scatter_kernel, dim3((rows + 31) / 32, (D + 63) / 64), 256, st, s, (uint16_t*)dhidden, dhidden_stride, D);
+    const dim3 grid((rows + 31) / 32, (D + 63) / 64);
+    return s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
+                         : launch_after(ce_scatter_kernel<1>, grid, 256, st, s, (uint16_t*)dhidden, dhidden_stride, D);
 }
