@@ -26,38 +26,80 @@ struct NormParams {
     float eps;
 };
 
-// The code of v as a float.  Adding and taking away 1.5 * 2^23 rounds to the nearest integer, ties to even, at the rate of
-// an addition (the conversion instructions run at an eighth of it).
-constexpr float kRounder = 12582912.f;
-__device__ __forceinline__ float code_of(float v, float top, float inv) {
-    const float t = v * inv;
-    float c = __fadd_rn(__fadd_rn(t, kRounder), -kRounder);
-    // A NaN t (v or top not finite, or top so small that inv overflowed) fails the comparison too.
-    if (!(fabsf(t - c) < 0.4999f)) {
-        const double e = rint(127.0 * (double)v / (double)top);
-        c = e == e ? fminf(fmaxf((float)e, -127.f), 127.f) : 0.f;
-    }
-    return c;
+// ---- pairs of fp32: one instruction for two elements (the kernel is bound by instructions before it is bound by memory) ----
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
 }
-
-// fp32 -> storage type, round to nearest even (bf16 patterns built by hand would cost more than the conversion)
-template <typename T> __device__ __forceinline__ void add_round(float* a, const float* b);
-template <> __device__ __forceinline__ void add_round<float>(float* a, const float* b) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = __fadd_rn(a[i], b[i]);
+__device__ __forceinline__ float lo_of(Pair p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float hi_of(Pair p) { return __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
 }
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {  // lo in the low half
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-template <> __device__ __forceinline__ void add_round<bf16_t>(float* a, const float* b) {
+
+// A 16-byte vector as pairs, and back (values that came from the storage type).
+template <typename T> __device__ __forceinline__ void to_pairs(const uint4& v, Pair* z);
+template <> __device__ __forceinline__ void to_pairs<float>(const uint4& v, Pair* z) {
+    z[0] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+    z[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+}
+template <> __device__ __forceinline__ void to_pairs<bf16_t>(const uint4& v, Pair* z) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        const uint32_t d = pack_bf16x2(__fadd_rn(a[i], b[i]), __fadd_rn(a[i + 1], b[i + 1]));
-        a[i] = __uint_as_float(d << 16);
-        a[i + 1] = __uint_as_float(d & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) z[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+// x + r rounded to the storage type, as a vector.
+template <typename T> __device__ __forceinline__ uint4 add_vec(const uint4& x, const uint4& r);
+template <> __device__ __forceinline__ uint4 add_vec<float>(const uint4& x, const uint4& r) {
+    return make_uint4(__float_as_uint(__fadd_rn(__uint_as_float(x.x), __uint_as_float(r.x))), __float_as_uint(__fadd_rn(__uint_as_float(x.y), __uint_as_float(r.y))),
+                      __float_as_uint(__fadd_rn(__uint_as_float(x.z), __uint_as_float(r.z))), __float_as_uint(__fadd_rn(__uint_as_float(x.w), __uint_as_float(r.w))));
+}
+template <> __device__ __forceinline__ uint4 add_vec<bf16_t>(const uint4& x, const uint4& r) {
+    Pair a[4], b[4];
+    to_pairs<bf16_t>(x, a);
+    to_pairs<bf16_t>(r, b);
+    uint32_t d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Pair t = add2(a[i], b[i]);
+        d[i] = pack_bf16x2(lo_of(t), hi_of(t));
     }
+    return make_uint4(d[0], d[1], d[2], d[3]);
+}
+
+// Adding 1.5 * 2^23 rounds to the nearest integer, ties to even, at the rate of an addition (the conversion instructions
+// run at an eighth of it), and leaves the integer's two's complement in the low bits.
+constexpr float kRounder = 12582912.f;
+// The exact codes of P values, as bytes.
+template <int P> __device__ __noinline__ Pair exact_codes(Pair a, Pair b, Pair c, Pair d, float top) {
+    const Pair z[4] = {a, b, c, d};
+    Pair bytes = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const double e = rint(127.0 * (double)(i & 1 ? hi_of(z[i / 2]) : lo_of(z[i / 2])) / (double)top);
+        const int code = e == e ? (int)fmin(fmax(e, -127.0), 127.0) : 0;
+        bytes |= (Pair)(uint8_t)code << (8 * i);
+    }
+    return bytes;
 }
 
 // The vector of elements [at, at + kPerVec) of a row of D; past the row's end (its last vector may be short) zeros.
@@ -70,18 +112,18 @@ template <typename T> __device__ __forceinline__ uint4 load_elems(const void* ro
     for (int i = 0; i < P; ++i) z[i] = at + i < D ? Elt<T>::load(row, at + i) : 0.f;
     return pack_vec<T>(z);
 }
-template <typename T> __device__ __forceinline__ void store_elems(void* row, int at, int D, const float* z) {
+template <typename T> __device__ __forceinline__ void store_elems(void* row, int at, int D, const uint4& v) {
     constexpr int P = Elt<T>::kPerVec;
-    const uint4 v = pack_vec<T>(z);
     char* p = (char*)row + (size_t)at * Elt<T>::kBytes;
     if (at + P <= D) {
         *reinterpret_cast<uint4*>(p) = v;
     } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             if (at + i < D) {
-                if (Elt<T>::kBytes == 4) reinterpret_cast<float*>(p)[i] = z[i];
-                else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(__float_as_uint(z[i]) >> 16);
+                if (Elt<T>::kBytes == 4) reinterpret_cast<uint32_t*>(p)[i] = w[i & 3];
+                else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[(i / 2) & 3] >> (16 * (i & 1)));
             }
         }
     }
@@ -107,44 +149,35 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024) norm_
 #pragma unroll
         for (int j = 0; j < NV; ++j) wv[j] = load_elems<T>(p.w, (tid + j * nth) * P, p.D);
     }
-    float v[NV][P];
-    float sum = 0.f, top = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) unpack_vec<T>(xv[j], v[j]);
     if (kNorm && r) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float b[P];
-            unpack_vec<T>(rv[j], b);
-            add_round<T>(v[j], b);
-        }
+        for (int j = 0; j < NV; ++j) xv[j] = add_vec<T>(xv[j], rv[j]);
     }
     if (kNorm && p.h) {
         char* h = (char*)p.h + row * p.hs * Elt<T>::kBytes;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int at = (tid + j * nth) * P;
-            if (at < p.D) store_elems<T>(h, at, p.D, v[j]);
+            if (at < p.D) store_elems<T>(h, at, p.D, xv[j]);
         }
     }
+    Pair v[NV][P / 2], squares = pair(0.f, 0.f);
+    float top = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        if (kNorm) {
+        to_pairs<T>(xv[j], v[j]);
 #pragma unroll
-            for (int i = 0; i < P; ++i) sum = fmaf(v[j][i], v[j][i], sum);
-            if (p.w) {
-                float w[P];
-                unpack_vec<T>(wv[j], w);
+        for (int i = 0; i < P / 2; ++i) squares = fma2(v[j][i], kNorm ? v[j][i] : pair(0.f, 0.f), squares);  // (quantiser: a NaN or infinity shows)
+        if (kNorm && p.w) {
+            Pair w[P / 2];
+            to_pairs<T>(wv[j], w);
 #pragma unroll
-                for (int i = 0; i < P; ++i) v[j][i] = __fmul_rn(v[j][i], w[i]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i) sum += v[j][i] * 0.f;  // carries a NaN or infinity into the scale
+            for (int i = 0; i < P / 2; ++i) v[j][i] = mul2(v[j][i], w[i]);
         }
 #pragma unroll
-        for (int i = 0; i < P; ++i) top = fmaxf(top, fabsf(v[j][i]));
+        for (int i = 0; i < P / 2; ++i) top = fmaxf(top, fmaxf(fabsf(lo_of(v[j][i])), fabsf(hi_of(v[j][i]))));
     }
+    float sum = lo_of(squares) + hi_of(squares);
     sum = warp_sum(sum);
     top = warp_max(top);
     if ((tid & 31) == 0) {
@@ -163,21 +196,32 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024) norm_
     else s += sum;
     if (tid == 0) p.scale[row] = s;
     const float inv = top > 0.f ? 127.f / top : 0.f;
+    // a row with a NaN or an infinity in it, or so small that inv overflows, takes the fp64 quotient throughout
+    const bool odd = !(inv < 3e38f) || !(top < 3e38f) || !(sum - sum == 0.f);
     int8_t* q = p.q + row * p.qs;
+    const Pair inv2 = pair(inv, inv), up = pair(kRounder, kRounder), down = pair(-kRounder, -kRounder), minus = pair(-1.f, -1.f), s2 = pair(s, s);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int at = (tid + j * nth) * P;
         if (at >= p.D) break;
-        float c[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) c[i] = code_of(v[j][i], top, inv);
+        Pair c[P / 2];
         uint32_t b[P / 4];
+        float border = 0.f;
 #pragma unroll
-        for (int i = 0; i < P / 4; ++i) {  // the low byte of c + kRounder is the code
-            uint32_t k[4];
+        for (int i = 0; i < P / 2; ++i) {
+            const Pair t = mul2(v[j][i], inv2), r = add2(t, up);
+            c[i] = add2(r, down);
+            const Pair d = fma2(c[i], minus, t);
+            border = fmaxf(border, fmaxf(fabsf(lo_of(d)), fabsf(hi_of(d))));
+            const uint32_t two = __byte_perm(__float_as_uint(lo_of(r)), __float_as_uint(hi_of(r)), 0x0040);
+            b[i / 2] = i & 1 ? __byte_perm(b[i / 2], two, 0x5410) : two;
+        }
+        if (odd || border >= 0.4999f) {
+            const Pair e = exact_codes<P>(v[j][0], v[j][1], v[j][P / 2 - 2], v[j][P / 2 - 1], top);
+            b[0] = (uint32_t)e;
+            if (P == 8) b[P / 4 - 1] = (uint32_t)(e >> 32);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = __float_as_uint(__fadd_rn(c[4 * i + e], kRounder));
-            b[i] = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
+            for (int i = 0; i < P / 2; ++i) c[i] = pair((float)(int8_t)(e >> (16 * i)), (float)(int8_t)(e >> (16 * i + 8)));
         }
         if (at + P <= p.D) {
             if (P == 8) *reinterpret_cast<uint2*>(q + at) = make_uint2(b[0], b[P / 4 - 1]);
@@ -191,7 +235,10 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024) norm_
             uint16_t* y = p.y + row * p.ys + at;
             uint32_t o[P / 2];
 #pragma unroll
-            for (int i = 0; i < P / 2; ++i) o[i] = pack_bf16x2(c[2 * i] * s, c[2 * i + 1] * s);
+            for (int i = 0; i < P / 2; ++i) {
+                const Pair z = mul2(c[i], s2);
+                o[i] = pack_bf16x2(lo_of(z), hi_of(z));
+            }
             if (at + P <= p.D) {
                 if (P == 8) *reinterpret_cast<uint4*>(y) = make_uint4(o[0], o[1], o[P / 2 - 2], o[P / 2 - 1]);
                 else *reinterpret_cast<uint2*>(y) = make_uint2(o[0], o[1]);
@@ -210,7 +257,7 @@ template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cu
     const int nvec = (p.D + Elt<T>::kPerVec - 1) / Elt<T>::kPerVec;
     // Few rows: latency counts, so a row is spread over as many threads as it has vectors.  Rows enough to fill the
     // machine: several vectors in flight per thread.
-    int nv = p.rows < 2 * 148 ? 1 : (nvec >= 256 ? 2 : 1);
+    int nv = p.rows < 2 * 148 ? 1 : (nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1);
     while ((nvec + nv - 1) / nv > 1024) nv *= 2;
     const int threads = ((nvec + nv - 1) / nv + 31) / 32 * 32;
     if (nv == 1) norm_quant_kernel<T, 1, kNorm><<<p.rows, threads, 0, st>>>(p);
