@@ -660,34 +660,16 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         const GradEpilogue::Params eg = {log2e_for(D), s.g, s.lse2, s.weight, s.target, s.rows_pad, (int)v0, (int)width};
         if (const int rc = product<GradEpilogue, 8>(s.pair, ta, tb, p, eg, st)) return rc;
 
-        // dW of the piece: rows are vocabulary entries, the sum runs over the rows that count
-        p.m_tiles = (int)(up(width, tile_rows) / tile_rows);
+        // the piece's part of dH first, while the weight's piece is still in L2 from the product above: the sum runs over the
+        // piece's vocabulary entries
+        const int ctas = s.pair ? 2 : 1, b_blocks = nt / ctas / 64;
+        const uint16_t* wp = w + v0 * weight_stride;
+        p.m_tiles = (int)(up(rows, tile_rows) / tile_rows);
         p.n_tiles = (D + nt - 1) / nt;
         p.nt = nt;
-        p.k_blocks = (int)(s.rows_pad / 64);
-        p.group_m = 8;
-        p.a_layout = p.b_layout = gemm::kBlocksMN;
-        p.m_total = (int)width;
-        p.m_limit = nullptr;
-        p.k_limit = s.count;
-        const int ctas = s.pair ? 2 : 1, b_blocks = nt / ctas / 64;
-        if (!gemm::encode_blocks(&ta, s.g, s.rows_pad, 128, s.piece / 64, s.rows_pad * 128, 2) ||
-            !gemm::encode_blocks(&tb, s.hidden, s.rows_pad, 128, s.ds / 64, s.rows_pad * 128, b_blocks))
-            return TSLT_ERR_CUDA;
-        uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
-        WeightEpilogue::Params ew = {{}, dw, dweight_stride, s.top_weight, (int)width, D};
-        if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
-        if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
-
-        // the piece's part of dH: the sum runs over its vocabulary entries
-        p.m_tiles = (int)(up(rows, tile_rows) / tile_rows);
         p.k_blocks = (int)((width + 63) / 64);
         p.splits = s.splits;
-        p.a_layout = gemm::kPanelsK;
-        p.m_total = rows;
-        p.m_limit = s.count;
-        p.k_limit = nullptr;
-        const uint16_t* wp = w + v0 * weight_stride;
+        p.group_m = 8;
         p.b_layout = D % 64 == 0 ? gemm::kBlocksMN : gemm::kRowsMN;
         if (!gemm::encode_map(&ta, gemm::kElemBf16, s.g, 64, s.piece / 64 * s.rows_pad, 128, 128) ||
             !(D % 64 == 0 ? gemm::encode_blocks(&tb, wp, width, weight_stride * 2, D / 64, 128, b_blocks)
@@ -695,6 +677,22 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
             return TSLT_ERR_CUDA;
         const HiddenEpilogue::Params eh = {(float4*)s.acc, s.rows_pad, s.da, D, c == 0};
         if (const int rc = product<HiddenEpilogue, 4>(s.pair, ta, tb, p, eh, st)) return rc;
+
+        // dW of the piece: rows are vocabulary entries, the sum runs over the rows that count
+        p.m_tiles = (int)(up(width, tile_rows) / tile_rows);
+        p.k_blocks = (int)(s.rows_pad / 64);
+        p.splits = 1;
+        p.a_layout = p.b_layout = gemm::kBlocksMN;
+        p.m_total = (int)width;
+        p.m_limit = nullptr;
+        p.k_limit = s.count;
+        if (!gemm::encode_blocks(&ta, s.g, s.rows_pad, 128, s.piece / 64, s.rows_pad * 128, 2) ||
+            !gemm::encode_blocks(&tb, s.hidden, s.rows_pad, 128, s.ds / 64, s.rows_pad * 128, b_blocks))
+            return TSLT_ERR_CUDA;
+        uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
+        WeightEpilogue::Params ew = {{}, dw, dweight_stride, s.top_weight, (int)width, D};
+        if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
+        if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
     }
     const dim3 grid((rows + 31) / 32, (D + 63) / 64);
     return s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
