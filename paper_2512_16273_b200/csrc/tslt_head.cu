@@ -1,6 +1,11 @@
 // The head product in 8-bit integers (tslt_head_logits): z[n, v] = s_n t_v sum_k q[n, k] c[v, k].  The sum is exact (32-bit
 // integers); the scales are multiplied in fp32 and the logit is rounded once.
 //
+// One to four rows (a draft's step): bound by reading the weight once and by how soon that starts.  No tensor cores: warps take
+// blocks of four weight rows, each lane 16 bytes of k at a time from all four, and dot products of four bytes (dp4a) with
+// the tokens' codes in shared memory.  V = 32000, K = 2048, us with / without this form: 1 row 14.4 / 18.8, 4 rows
+// 15.8 / 18.8, 8 rows 23.0 / 19.4 (the dot products are then the bound); V = 128256, K = 4096: 1 row 80 / 87, 4 rows 83 / 91.
+//
 // Few rows (a decoding step): bound by reading the weight once.  The weight is the operand of the tensor cores' 128 rows and
 // the tokens are its columns (16 ... 128), so that the whole weight goes once through shared memory whatever their number.
 //
@@ -118,12 +123,113 @@ template <typename T> struct HeadRowsEpilogue {
     }
 };
 
+// One to four rows.  kRows: 1, 2 or 4, the rows of q in shared memory (rows of zeros behind the last).
+constexpr int kVecBlock = 4;  // weight rows of a warp at a time
+constexpr int kVecThreads = 256;
+constexpr int kVecCodes = 40 * 1024;  // most bytes of q in shared memory
+struct VecParams {
+    const int8_t *q, *w;
+    const float *row_scale, *weight_scale;
+    void* out;
+    long long q_stride, w_stride, out_stride;
+    int rows, V, K;
+    int* status;
+};
+template <int kRows, typename T>
+__global__ void __launch_bounds__(kVecThreads, 4) head_vec_kernel(const __grid_constant__ VecParams p) {
+    extern __shared__ __align__(16) uint8_t s_codes[];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int chunks = (p.K + 15) / 16;  // a row's last 16 bytes may hold anything behind K: they meet zeros
+    if (blockIdx.x == 0 && tid == 0) *p.status = 0;  // nothing here waits
+    for (int i = tid; i < kRows * chunks; i += kVecThreads) {
+        const int r = i / chunks, at = (i - r * chunks) * 16;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < p.rows) {
+            v = *reinterpret_cast<const uint4*>(p.q + r * p.q_stride + at);
+            if (at + 16 > p.K) {  // zeros behind the last code
+                uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int n = p.K - at - 4 * j;  // codes left in this word
+                    w[j] = n >= 4 ? w[j] : n <= 0 ? 0u : w[j] & ((1u << (8 * n)) - 1u);
+                }
+            }
+        }
+        reinterpret_cast<uint4*>(s_codes)[i] = v;
+    }
+    __syncthreads();
+    const uint4* codes = reinterpret_cast<const uint4*>(s_codes);
+    const int warps = gridDim.x * (kVecThreads / 32);
+    for (long long v0 = (long long)(blockIdx.x * (kVecThreads / 32) + (tid >> 5)) * kVecBlock; v0 < p.V; v0 += (long long)warps * kVecBlock) {
+        int acc[kVecBlock][kRows];
+#pragma unroll
+        for (int b = 0; b < kVecBlock; ++b)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) acc[b][r] = 0;
+        const int8_t* w[kVecBlock];
+#pragma unroll
+        for (int b = 0; b < kVecBlock; ++b) w[b] = p.w + (v0 + b < p.V ? v0 + b : p.V - 1) * p.w_stride;
+        for (int c0 = lane; c0 < chunks; c0 += 64) {  // eight loads in flight
+            uint4 x[2][kVecBlock];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int b = 0; b < kVecBlock; ++b)
+                    x[u][b] = c0 + 32 * u < chunks ? __ldcs(reinterpret_cast<const uint4*>(w[b]) + c0 + 32 * u) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const uint4 q = codes[r * chunks + (c0 + 32 * u < chunks ? c0 + 32 * u : lane)];
+#pragma unroll
+                    for (int b = 0; b < kVecBlock; ++b) {
+                        acc[b][r] = __dp4a((int)x[u][b].x, (int)q.x, acc[b][r]);
+                        acc[b][r] = __dp4a((int)x[u][b].y, (int)q.y, acc[b][r]);
+                        acc[b][r] = __dp4a((int)x[u][b].z, (int)q.z, acc[b][r]);
+                        acc[b][r] = __dp4a((int)x[u][b].w, (int)q.w, acc[b][r]);
+                    }
+                }
+            }
+        }
+        // lane 4 r + b ends up with the sum of row r and weight row b
+        int mine = 0;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int b = 0; b < kVecBlock; ++b) {
+                const int sum = __reduce_add_sync(0xffffffffu, acc[b][r]);
+                if (lane == r * kVecBlock + b) mine = sum;
+            }
+        const int r = lane / kVecBlock;
+        const long long v = v0 + lane % kVecBlock;
+        if (r < kRows && r < p.rows && v < p.V) {
+            const float z = (float)mine * __ldg(p.row_scale + r) * __ldg(p.weight_scale + v);
+            HeadEpilogue<T>::put(reinterpret_cast<T*>(p.out) + r * p.out_stride + v, z);
+        }
+    }
+}
+
+template <int kRows, typename T> static int launch_vec(VecParams p, int* status, cudaStream_t st) {
+    p.status = status;
+    const long long blocks = ((long long)p.V + kVecBlock * (kVecThreads / 32) - 1) / (kVecBlock * (kVecThreads / 32));
+    const int sms = gemm::sm_count();
+    if (sms <= 0) return TSLT_ERR_CUDA;
+    const long long most = (long long)sms * 4;
+    head_vec_kernel<kRows, T><<<(unsigned)(blocks < most ? blocks : most), kVecThreads, (size_t)kRows * ((p.K + 15) / 16 * 16), st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+}
+
 // Rows from which the tokens become the tensor cores' rows.
 constexpr int kManyRows = 129;
 
 template <typename T>
 static int launch_head(const signed char* q, const float* qs, long long q_stride, const signed char* w, const float* ws, long long w_stride,
                        int rows, int V, int K, T* out, long long out_stride, int* status, cudaStream_t st) {
+    const int vec_rows = rows <= 2 ? rows : 4;
+    if (rows <= 4 && vec_rows * K <= kVecCodes) {
+        const VecParams v = {(const int8_t*)q, (const int8_t*)w, qs, ws, out, q_stride, w_stride, out_stride, rows, V, K};
+        return vec_rows == 1 ? launch_vec<1, T>(v, status, st) : vec_rows == 2 ? launch_vec<2, T>(v, status, st) : launch_vec<4, T>(v, status, st);
+    }
     gemm::Product p = {};
     p.splits = 1;
     p.k_elems = 128;

@@ -489,20 +489,31 @@ __global__ void __launch_bounds__(256 * kGroups) ce_scatter_kernel(CeSpace s, ui
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 7, group = threadIdx.x >> 8;
     const float4* acc = reinterpret_cast<const float4*>(s.acc);
     const int from = s.splits * group / kGroups, to = s.splits * (group + 1) / kGroups;
+    const long long cut = s.da / 4 * s.rows_pad;
+    const float4* a[2];
+    bool on[2];
     float4 v[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int c4 = warp + 8 * k, d = d0 + 4 * c4;
+        const int d = d0 + 4 * (warp + 8 * k);
+        on[k] = d < D && r0 + lane < rows;
+        a[k] = acc + (long long)(d / 4) * s.rows_pad + r0 + lane;
         v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (d < D && r0 + lane < rows) {
-            const float4* a = acc + (long long)(d / 4) * s.rows_pad + r0 + lane;
-#pragma unroll 8
-            for (int i = from; i < to; ++i) {
-                const float4 w = a[i * (s.da / 4) * s.rows_pad];
-                v[k] = make_float4(v[k].x + w.x, v[k].y + w.y, v[k].z + w.z, v[k].w + w.w);
-            }
-        }
-        if (group > 0) sums[group - 1][c4][lane] = v[k];
+    }
+    for (int i = from; i < to; i += 4) {  // eight loads in flight
+        float4 w[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[k][j] = on[k] && i + j < to ? a[k][(i + j) * cut] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[k] = make_float4(v[k].x + w[k][j].x, v[k].y + w[k][j].y, v[k].z + w[k][j].z, v[k].w + w[k][j].w);
+    }
+    if (group > 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sums[group - 1][warp + 8 * k][lane] = v[k];
     }
     if (kGroups > 1) __syncthreads();
     if (group == 0) {

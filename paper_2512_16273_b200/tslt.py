@@ -945,11 +945,20 @@ def head_logits(q: torch.Tensor, scale: torch.Tensor, weight: torch.Tensor, weig
     _vector(weight_scale, "weight_scale", torch.float32, dev, V)
     if logits_dtype not in (torch.float32, torch.bfloat16):
         raise TsltError(ERR_UNSUPPORTED, "dtype %s" % logits_dtype)
-    o = {} if out is None else out
-    z = _given(o, "logits", (*q.shape[:-1], V), logits_dtype, dev)
-    if z is None:
-        z = o["logits"] = _rows_like(q.shape[:-1], V, logits_dtype, device)
-    zs = _stride(z, V, "logits")
+    if out is None:
+        step = _STEP[logits_dtype]
+        zs = -(-V // step) * step
+        if zs == V and q.dim() == 2:
+            z = torch.empty(rows, V, dtype=logits_dtype, device=device)
+        else:
+            z = _rows_like(q.shape[:-1], V, logits_dtype, device)
+        o = {"logits": z}
+    else:
+        o = out
+        z = _given(o, "logits", (*q.shape[:-1], V), logits_dtype, dev)
+        if z is None:
+            z = o["logits"] = _rows_like(q.shape[:-1], V, logits_dtype, device)
+        zs = _stride(z, V, "logits")
     ws = _space(ws, 256, device, dev)
     _check(lib().tslt_head_logits(_at(q), _at(scale), qs, _at(weight), _at(weight_scale), wstride, rows, V, D,
                                   F32 if logits_dtype == torch.float32 else BF16, _at(z), zs, _at(ws), ws.numel(), _stream_on(dev)),
