@@ -175,6 +175,12 @@ def _stream() -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _whole(n: int, t: torch.Tensor) -> int:
+    """n elements rounded up to a multiple of 16 bytes."""
+    step = max(1, 16 // t.element_size())
+    return -(-n // step) * step
+
+
 def _row_layout(logits: torch.Tensor):
     """(rows, V, row stride in elements) of a tensor [..., V] whose leading dimensions flatten
     to equally spaced rows (a contiguous tensor, or a [:, ..., :V] view of a padded one)."""
@@ -183,14 +189,14 @@ def _row_layout(logits: torch.Tensor):
     V = logits.shape[-1]
     rows = logits.numel() // V if V else 0
     if logits.dim() == 1:
-        return rows, V, V
+        return rows, V, _whole(V, logits)
     stride = logits.stride(-2)
     for d in range(logits.dim() - 2):
         if logits.shape[d] > 1 and logits.stride(d) != logits.stride(d + 1) * logits.shape[d + 1]:
             raise ValueError("rows of logits must be equally spaced in memory")
     if rows <= 1 or logits.shape[-2] == 1:
         # a single row per block: take the spacing from the next dimension that has one
-        stride = V
+        stride = _whole(V, logits)  # of one row in all, no spacing is ever used
         for d in range(logits.dim() - 2, -1, -1):
             if logits.shape[d] > 1:
                 stride = logits.stride(d)

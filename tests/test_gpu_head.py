@@ -227,3 +227,233 @@ def test_linear_ce_backward(rows, V, D, ignored):
     assert tslt.workspace_status(g["workspace"]) == 0
     again = tslt.linear_ce_backward(hp, wp, t, f["lse"], dl)
     assert torch.equal(again["dhidden"], g["dhidden"]) and torch.equal(again["dweight"], g["dweight"])
+
+
+def test_linear_ce_several_pieces():
+    """Rows and vocabulary at which the backward cuts the vocabulary in pieces, and dH's sum in cuts."""
+    rows, V, D = 3000, 70000, 136
+    assert tslt.linear_ce_backward_workspace_bytes(rows, V, D) < rows * V * 2  # less than the logits in 16 bits
+    h, w, t, dl = loss_case(rows, V, D, 0.2, 3)
+    d, b = loss_reference(h, w, t, dl)
+    f = tslt.linear_ce(h, w, t)
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+    for k, o in (("loss", f), ("lse", f)):
+        within(o[k], d[k], torch.where(t >= 0, b[k], torch.zeros_like(b[k])), k)
+    for k in ("dhidden", "dweight"):
+        within(g[k], d[k], b[k], k)
+
+
+@pytest.mark.parametrize("rows", [1, 300])
+def test_linear_ce_no_row_counts(rows):
+    V, D = 777, 96
+    h = torch.full((rows, D), float("nan"), device="cuda", dtype=BF16)
+    w = torch.randn(V, D, device="cuda").to(BF16)
+    t = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    f = tslt.linear_ce(h, w, t)
+    g = tslt.linear_ce_backward(h, w, t, f["lse"])
+    assert not f["loss"].any() and not f["lse"].any() and not g["dhidden"].any() and not g["dweight"].any()
+    assert g["dweight"].isfinite().all() and g["dhidden"].isfinite().all()
+
+
+def test_empty_batches():
+    w = torch.randn(50, 64, device="cuda").to(BF16)
+    h, t = w[:0], torch.zeros(0, dtype=torch.int32, device="cuda")
+    f = tslt.linear_ce(h, w, t)
+    out = {"dweight": torch.full((50, 64), 3.0, dtype=BF16, device="cuda")}
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], out=out)
+    assert f["loss"].shape == (0,) and g["dhidden"].shape == (0, 64) and not g["dweight"].any()
+    n = tslt.rmsnorm_quant(h, w[0], h)
+    assert n["q"].shape == (0, 64)
+    c = tslt.quantize_rows(w)
+    assert tslt.head_logits(n["q"], n["scale"], c["q"], c["scale"])["logits"].shape == (0, 50)
+
+
+def test_targets_behind_the_vocabulary_are_ignored_and_reported():
+    h, w, t, dl = loss_case(20, 100, 64, 0.0, 9)
+    bad = t.clone()
+    bad[3] = 100
+    bad[7] = 2 ** 31 - 1
+    f = tslt.linear_ce(h, w, bad)
+    assert tslt.workspace_status(f["workspace"]) == tslt.STATUS_BAD_TARGET
+    ok = torch.where(bad == t, t, -1)
+    assert torch.equal(f["loss"], tslt.linear_ce(h, w, ok)["loss"]) and f["loss"][3] == 0
+    g = tslt.linear_ce_backward(h, w, bad, f["lse"], dl)
+    assert tslt.workspace_status(g["workspace"]) == tslt.STATUS_BAD_TARGET
+    want = tslt.linear_ce_backward(h, w, ok, f["lse"], dl)
+    assert torch.equal(g["dhidden"], want["dhidden"]) and torch.equal(g["dweight"], want["dweight"])
+    assert tslt.workspace_status(want["workspace"]) == 0  # cleared by the next call
+
+
+def test_linear_ce_not_finite():
+    """A NaN or an infinity in a row that counts shows in that row's outputs and in no other row's."""
+    h, w, t, _ = loss_case(40, 333, 128, 0.0, 4)
+    good = tslt.linear_ce(h, w, t)
+    h[5, 3] = float("nan")
+    h[9, 0] = float("inf")
+    f = tslt.linear_ce(h, w, t)
+    rest = torch.ones(40, dtype=torch.bool, device="cuda")
+    rest[[5, 9]] = False
+    assert not f["loss"][5].isfinite() and not f["loss"][9].isfinite()
+    assert torch.equal(f["loss"][rest], good["loss"][rest]) and torch.equal(f["lse"][rest], good["lse"][rest])
+    g = tslt.linear_ce_backward(h, w, t, f["lse"])
+    assert g["dhidden"][rest].isfinite().all() and not g["dhidden"][5].isfinite().any()
+
+
+def test_linear_ce_equal_weights_are_a_common_factor():
+    """The largest weight is taken out of the 16-bit gradients of the logits: equal weights scale the gradients exactly."""
+    h, w, t, _ = loss_case(150, 999, 256, 0.3, 6)
+    f = tslt.linear_ce(h, w, t)
+    one = tslt.linear_ce_backward(h, w, t, f["lse"])
+    third = tslt.linear_ce_backward(h, w, t, f["lse"], torch.full((150,), 0.25, device="cuda"))
+    for k in ("dhidden", "dweight"):
+        assert torch.equal(one[k] * 0.25, third[k])
+
+
+def test_linear_ce_gradient_against_differences():
+    """Directional differences of the 64-bit loss against the kernels' gradients."""
+    rows, V, D = 60, 500, 96
+    h, w, t, dl = loss_case(rows, V, D, 0.2, 12)
+    f = tslt.linear_ce(h, w, t)
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+    _, b = loss_reference(h, w, t, dl)
+    on = t >= 0
+
+    def total(hd, wd):
+        z = hd[on] @ wd.T
+        loss = torch.logsumexp(z, 1) - z.gather(1, t[on].long()[:, None])[:, 0]
+        return float((loss * dl[on].double()).sum())
+    r = gen(1)
+    step = 1e-5
+    for k, i in (("dhidden", 0), ("dweight", 1)):
+        for _ in range(3):
+            x = [h.double(), w.double()]
+            e = torch.randn(x[i].shape, device="cuda", generator=r, dtype=torch.float64)
+            lo, hi = list(x), list(x)
+            lo[i], hi[i] = x[i] - step * e, x[i] + step * e
+            diff = (total(*hi) - total(*lo)) / (2 * step)
+            got = float((g[k].double() * e).sum())
+            # each element's bound, and the difference quotient's own error (step^2 of a smooth function, and cancellation)
+            assert abs(got - diff) <= float((b[k] * e.abs()).sum()) + 1e-6 * (1 + abs(diff))
+
+
+# ---- large offsets, graphs, streams, the run together --------------------------------------------------------
+def test_weights_of_more_than_2_31_elements():
+    V, D = 540000, 4096
+    g = gen(2)
+    w = torch.randint(-127, 128, (V, D), device="cuda", generator=g, dtype=torch.int8)
+    t = torch.rand(V, device="cuda", generator=g)
+    for rows in (2, 20, 140):
+        q = torch.randint(-127, 128, (rows, D), device="cuda", generator=g, dtype=torch.int8)
+        s = torch.rand(rows, device="cuda", generator=g)
+        z = tslt.head_logits(q, s, w, t, F32)["logits"]
+        for v in (0, 1000, 524287, 524288, V - 1000):
+            want = (q.double() @ w[v:v + 1000].double().T) * s.double()[:, None] * t[v:v + 1000].double()[None, :]
+            within(z[:, v:v + 1000], want, want.abs() * (3 * U32 * 1.01) + 1e-40, "logits")
+    del w, z
+    V, D, rows = 140000, 16384, 20
+    w = (torch.randn(V, D, device="cuda", generator=g) * 0.01).to(BF16)
+    h = torch.randn(rows, D, device="cuda", generator=g).to(BF16)
+    t = torch.randint(V - 2000, V, (rows,), device="cuda", generator=g).to(torch.int32)
+    f = tslt.linear_ce(h, w, t)
+    z = torch.cat([h.double() @ w[v:v + 20000].double().T for v in range(0, V, 20000)], 1)
+    lse = torch.logsumexp(z, 1)
+    # as loss_reference's bounds, with the logits' own magnitudes
+    dz = max(float((h.abs().double() @ w[v:v + 20000].abs().double().T).max()) for v in range(0, V, 20000)) * (D + 16) * 2 * U32
+    within(f["lse"], lse, 3 * dz + 2.0 ** -20 + lse.abs() * 4 * U32, "lse")
+    b = tslt.linear_ce_backward(h, w, t, f["lse"])
+    gr = torch.exp(z - lse[:, None])
+    gr[torch.arange(rows, device="cuda"), t.long()] -= 1
+    for v in (0, 131071, V - 2000):
+        want, mag = gr[:, v:v + 2000].T @ h.double(), gr[:, v:v + 2000].abs().T @ h.double().abs()
+        within(b["dweight"][v:v + 2000], want, mag * (UBF + 4 * dz + 2.0 ** -18) * 1.01 + UBF * want.abs() + 1e-30, "dweight")
+
+
+def test_two_captured_graphs_do_not_share_a_workspace():
+    cases = [loss_case(90, 1500, 256, 0.2, s) for s in (21, 22)]
+    want = []
+    for h, w, t, dl in cases:
+        f = tslt.linear_ce(h, w, t)
+        g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+        want.append((f["loss"].clone(), g["dhidden"].clone(), g["dweight"].clone()))
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for h, w, t, dl in cases:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            f = tslt.linear_ce(h, w, t)
+            g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+        graphs.append(gr)
+        outs.append((f["loss"], g["dhidden"], g["dweight"]))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(10):
+        for gr, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                gr.replay()
+    torch.cuda.synchronize()
+    for o, x in zip(outs, want):
+        assert all(torch.equal(a, b) for a, b in zip(o, x))
+    # new inputs in the captured buffers
+    h, w, t, dl = cases[0]
+    h2, w2, t2, dl2 = loss_case(90, 1500, 256, 0.5, 23)
+    f = tslt.linear_ce(h2, w2, t2)
+    g = tslt.linear_ce_backward(h2, w2, t2, f["lse"], dl2)
+    for a, b in ((h, h2), (w, w2), (t, t2), (dl, dl2)):
+        a.copy_(b)
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs[0], (f["loss"], g["dhidden"], g["dweight"])))
+
+
+def test_calls_on_two_streams_at_once():
+    q, w, s, t, _ = head_case(200, 30000, 512, 31)
+    h, lw, lt, _ = loss_case(200, 3000, 512, 0.1, 32)
+    z = tslt.head_logits(q, s, w, t)["logits"].clone()
+    loss = tslt.linear_ce(h, lw, lt)["loss"].clone()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(8):
+        with torch.cuda.stream(a):
+            got.append((tslt.head_logits(q, s, w, t)["logits"], z))
+            got.append((tslt.linear_ce(h, lw, lt)["loss"], loss))
+        with torch.cuda.stream(b):
+            got.append((tslt.linear_ce(h, lw, lt)["loss"], loss))
+            got.append((tslt.head_logits(q, s, w, t)["logits"], z))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in got)
+
+
+@pytest.mark.parametrize("logits", [F32, BF16])
+@pytest.mark.parametrize("B,gamma", [(1, 1), (1, 4), (7, 3), (40, 5)])
+def test_from_hidden_states_to_drafts_and_verification(B, gamma, logits):
+    """norm -> head -> sparsify on the draft's side, norm -> head -> verify on the target's, as they are used together."""
+    import oracle
+    from paper_2512_16273_b200 import synth
+    from parity_utils import compare_sparsify, compare_verify, verify_inputs
+    V, D, k, T = 3001, 320, 32, 0.9
+    g = gen(B * 10 + gamma)
+    w = tslt.quantize_rows((torch.randn(V, D, device="cuda", generator=g) * (3 / math.sqrt(D))).to(BF16))
+    nw = (1 + 0.1 * torch.randn(D, device="cuda", generator=g)).to(BF16)
+    x, r = (torch.randn(B, gamma, D, device="cuda", generator=g).to(BF16) for _ in range(2))
+    ud = synth.uniforms((B * gamma, 1), 0, synth.TID_U_DRAFT)
+    s = tslt.sparsify_hidden(x, nw, w["q"], w["scale"], k, 1.0, T, ud.cuda(), residual=r, logits_dtype=logits)
+    h, q, scale = norm_reference(x.reshape(-1, D), r.reshape(-1, D), nw, 1e-6)
+    assert s["logits"].shape == (B, gamma, V) and torch.equal(s["residual"].reshape(-1, D), h)
+    z = (q @ w["q"].double().T) * scale[:, None] * w["scale"].double()[None, :]
+    within(s["logits"].reshape(-1, V), z, z.abs() * ((D / 2 + 12) * U32 + (UBF if logits == BF16 else 0)) * 1.01 + 1e-40, "logits")
+    zq = s["logits"].reshape(-1, V).cpu()
+    ref = oracle.sparsify(zq, k, 1.0, T, ud.numpy())
+    compare_sparsify(s, ref, "hidden", logits=zq, uniforms=ud, T=T)
+    # the target: one more row a sequence
+    xt = torch.cat([x + 0.1 * torch.randn(x.shape, device="cuda", generator=g).to(BF16), x[:, :1]], 1)
+    n = tslt.rmsnorm_quant(xt, nw, torch.cat([r, r[:, :1]], 1))
+    zt = tslt.head_logits(n["q"], n["scale"], w["q"], w["scale"], logits)["logits"]
+    ua = synth.uniforms((B, gamma), 0, synth.TID_U_ACCEPT)
+    us = synth.uniforms((B,), 0, synth.TID_U_SAMPLE)
+    tok = np.ascontiguousarray(ref["token"][:, 0].reshape(B, gamma))
+    v = tslt.verify(zt, s["idx"].view(B, gamma, k), s["logit"].view(B, gamma, k), s["count"].view(B, gamma), torch.from_numpy(tok).cuda(),
+                    T, T, ua.cuda(), us.cuda())
+    zc = zt.cpu()
+    rv = oracle.verify(zc, ref["idx"].reshape(B, gamma, k), ref["logit"].reshape(B, gamma, k), ref["count"].reshape(B, gamma), tok, T, T,
+                       ua.numpy(), us.numpy())
+    compare_verify(v, rv, "hidden", inputs=verify_inputs(zc, ref, B, gamma, k, tok, T, T, ua, us))
