@@ -568,14 +568,16 @@ static int product(bool pair, const CUtensorMap& ta, const CUtensorMap& tb, cons
     return pair ? gemm::launch<false, 2, kWarps, Epi>(ta, tb, p, ep, true, st) : gemm::launch<false, 1, kWarps, Epi>(ta, tb, p, ep, true, st);
 }
 
-// z of `width` vocabulary entries from row v0 of the weight: the product that forward and backward share.
-static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, long long w_stride, long long width, int nt, gemm::Product* p,
+// z of `width` vocabulary entries of the weight, in tiles that reach column `cover` at least: the product that forward and
+// backward share.
+static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, long long w_stride, long long width, long long cover, int nt,
+                          gemm::Product* p,
                           CUtensorMap* ta, CUtensorMap* tb) {
     *p = gemm::Product{};
     const int tile_rows = s.pair ? 256 : 128;
     p->m_tiles = (int)(up(rows, tile_rows) / tile_rows);
     p->nt = nt;
-    p->n_tiles = (int)((width + nt - 1) / nt);
+    p->n_tiles = (int)((cover + nt - 1) / nt);
     p->splits = 1;
     p->k_elems = 64;
     p->k_blocks = (D + 63) / 64;
@@ -634,7 +636,7 @@ extern "C" int tslt_linear_ce(const void* hidden, long long hidden_stride, const
     cudaStream_t st = (cudaStream_t)stream;
     gemm::Product p;
     CUtensorMap ta, tb;
-    if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, s.nt, &p, &ta, &tb)) return rc;
+    if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, V, s.nt, &p, &ta, &tb)) return rc;
     const GatherParams g = {(const uint16_t*)hidden, (const uint16_t*)weight, target, hidden_stride, weight_stride, rows, V, D, 0, nullptr,
                             nullptr, loss, lse, nullptr, 0, s};
     if (const int rc = gather(g, st)) return rc;
@@ -666,7 +668,7 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         const long long v0 = c * s.piece, width = v0 + s.piece < V ? s.piece : V - v0;
         gemm::Product p;
         CUtensorMap ta, tb;
-        if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width,
+        if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width, up(width, 64),  // dH sums in steps of 64
                                          gemm::choose_nt((rows + tile_rows - 1) / tile_rows, width, s.pair != 0, 32), &p, &ta, &tb)) return rc;
         const GradEpilogue::Params eg = {log2e_for(D), s.g, s.lse2, s.weight, s.target, s.rows_pad, (int)v0, (int)width};
         if (const int rc = product<GradEpilogue, 8>(s.pair, ta, tb, p, eg, st)) return rc;

@@ -229,6 +229,22 @@ def test_linear_ce_backward(rows, V, D, ignored):
     assert torch.equal(again["dhidden"], g["dhidden"]) and torch.equal(again["dweight"], g["dweight"])
 
 
+@pytest.mark.parametrize("rows,V,D,ignored", LOSS_SHAPES + [(77, 32001, 1000, 0.1), (60, 225, 64, 0.0), (300, 24700, 200, 0.4)])
+def test_linear_ce_reads_nothing_it_has_not_written(rows, V, D, ignored):
+    """Workspaces full of NaN: the outputs are the same."""
+    h, w, t, dl = loss_case(rows, V, D, ignored, rows + V)
+    d, b = loss_reference(h, w, t, dl)
+
+    h, w = padded(h), padded(w)
+
+    def poison(n):
+        return torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    f = tslt.linear_ce(h, w, t, ws=poison(tslt.linear_ce_workspace_bytes(rows, V, D)))
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], dl, ws=poison(tslt.linear_ce_backward_workspace_bytes(rows, V, D)))
+    for k, o in (("loss", f), ("lse", f), ("dhidden", g), ("dweight", g)):
+        within(o[k], d[k], torch.where(t >= 0, b[k], torch.zeros_like(b[k])) if o is f else b[k], k)
+
+
 def test_linear_ce_several_pieces():
     """Rows and vocabulary at which the backward cuts the vocabulary in pieces, and dH's sum in cuts."""
     rows, V, D = 3000, 70000, 136
@@ -236,7 +252,8 @@ def test_linear_ce_several_pieces():
     h, w, t, dl = loss_case(rows, V, D, 0.2, 3)
     d, b = loss_reference(h, w, t, dl)
     f = tslt.linear_ce(h, w, t)
-    g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+    ws = torch.full((tslt.linear_ce_backward_workspace_bytes(rows, V, D),), 255, dtype=torch.uint8, device="cuda")
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], dl, ws=ws)
     for k, o in (("loss", f), ("lse", f)):
         within(o[k], d[k], torch.where(t >= 0, b[k], torch.zeros_like(b[k])), k)
     for k in ("dhidden", "dweight"):
