@@ -71,11 +71,11 @@ extern "C" {
 #define TSLT_MAX_SHARDS 16
 
 /* limits of the output head's calls: hidden size; hidden size of the 8-bit head product (its sums stay
- * inside 32 bits: 128 * 128 * 65536 = 2^30); rows and vocabulary of the loss */
+ * inside 32 bits: 128 * 128 * 65536 = 2^30); rows of the loss; vocabulary of both, and rows of the head product */
 #define TSLT_MAX_HIDDEN 16384
 #define TSLT_MAX_INT8_K 65536
 #define TSLT_MAX_LOSS_ROWS (1 << 20)
-#define TSLT_MAX_LOSS_VOCAB (1 << 24)
+#define TSLT_MAX_VOCAB (1 << 24)
 
 /* size of the scratch array built into the library for tslt_verify_static */
 #define TSLT_STATIC_SCRATCH_BYTES (8u << 20)
@@ -394,7 +394,8 @@ int tslt_quantize_rows(const void* x, int dtype, int rows, int D, long long x_st
  * weight_scale) and the result is rounded once to logits_dtype (TSLT_F32 or TSLT_BF16).  The logits are laid out as
  * tslt_sparsify, tslt_verify and tslt_tree_verify read them.
  * q [rows, D] and weight [V, D] int8 (-128 is allowed), logits [rows, V], each with a row stride (elements); base pointers
- * 16-byte aligned, strides multiples of 16 bytes; rows, V and D may be any numbers, D <= TSLT_MAX_INT8_K.  Elements between
+ * 16-byte aligned, strides multiples of 16 bytes; rows, V and D need not be multiples of anything; D <= TSLT_MAX_INT8_K, rows and
+ * V <= TSLT_MAX_VOCAB.  Elements between
  * V and logits_stride are left as they are.  Workspace >= 256 bytes (the status word), 256-byte aligned.
  */
 int tslt_head_logits(const signed char* q, const float* q_scale, long long q_stride, const signed char* weight,
@@ -415,7 +416,8 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  * own rounding); sums are fp32 and their order is fixed: the same inputs give the same bits.
  * hidden, dhidden [rows, D], weight, dweight [V, D]: bf16 with row strides (elements, multiples of 8), 16-byte aligned;
  * target [rows] int32; loss, lse, dloss [rows] fp32.  rows = 0 is allowed (dweight = 0).  D <= TSLT_MAX_HIDDEN, rows <=
- * TSLT_MAX_LOSS_ROWS, V <= TSLT_MAX_LOSS_VOCAB.  Outputs must not overlap inputs.
+ * TSLT_MAX_LOSS_ROWS, V <= TSLT_MAX_VOCAB.  Outputs must not overlap inputs or each other (the same
+ * pointer is refused).
  */
 int tslt_linear_ce_workspace_bytes(int rows, int V, int D, size_t* bytes);
 int tslt_linear_ce(const void* hidden, long long hidden_stride, const void* weight, long long weight_stride,

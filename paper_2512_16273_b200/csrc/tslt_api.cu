@@ -3,7 +3,7 @@
 
 #include "../../include/tslt.h"
 
-extern "C" int tslt_version(void) { return 100; }
+extern "C" int tslt_version(void) { return 200; }
 
 extern "C" const char* tslt_status_string(int status) {
     switch (status) {

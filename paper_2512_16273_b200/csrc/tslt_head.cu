@@ -270,7 +270,7 @@ extern "C" int tslt_head_logits(const signed char* q, const float* q_scale, long
                                 long long logits_stride, void* workspace, size_t workspace_bytes, void* stream) {
     if (logits_dtype != TSLT_F32 && logits_dtype != TSLT_BF16) return TSLT_ERR_UNSUPPORTED;
     if (rows < 0 || V <= 0 || D <= 0) return TSLT_ERR_INVALID_ARG;
-    if (D > TSLT_MAX_INT8_K) return TSLT_ERR_UNSUPPORTED;
+    if (D > TSLT_MAX_INT8_K || rows > TSLT_MAX_VOCAB || V > TSLT_MAX_VOCAB) return TSLT_ERR_UNSUPPORTED;
     if (rows == 0) return TSLT_OK;
     const int b = logits_dtype == TSLT_F32 ? 4 : 2;
     auto bad = [](const void* p, long long stride_bytes, long long row_bytes) {

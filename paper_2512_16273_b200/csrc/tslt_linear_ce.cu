@@ -603,7 +603,7 @@ static int check_common(const void* hidden, long long h_stride, const void* weig
 
 static int check_sizes(int rows, int V, int D) {
     if (rows < 0 || V <= 0 || D <= 0) return TSLT_ERR_INVALID_ARG;
-    if (D > TSLT_MAX_HIDDEN || rows > TSLT_MAX_LOSS_ROWS || V > TSLT_MAX_LOSS_VOCAB) return TSLT_ERR_UNSUPPORTED;
+    if (D > TSLT_MAX_HIDDEN || rows > TSLT_MAX_LOSS_ROWS || V > TSLT_MAX_VOCAB) return TSLT_ERR_UNSUPPORTED;
     return TSLT_OK;
 }
 
@@ -656,6 +656,7 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
     cudaStream_t st = (cudaStream_t)stream;
     if (rows == 0)  // no row contributes
         return cudaMemset2DAsync(dweight, dweight_stride * 2, 0, (size_t)D * 2, V, st) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    if (dhidden == hidden || dhidden == weight || dhidden == dweight || dweight == hidden || dweight == weight) return TSLT_ERR_INVALID_ARG;
     if (bad(dhidden, dhidden_stride) || !lse || !workspace || ((uintptr_t)workspace & 255)) return TSLT_ERR_INVALID_ARG;
     const CeSpace s = ce_space(workspace, rows, V, D, true);
     if (workspace_bytes < s.bytes) return TSLT_ERR_WORKSPACE;

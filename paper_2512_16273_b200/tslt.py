@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 import os
 from typing import Dict, Optional, Sequence
 
@@ -734,17 +735,20 @@ def diagnostics(draft_logits: torch.Tensor, target_logits: torch.Tensor, k_list:
 MAX_HIDDEN = 16384
 MAX_INT8_K = 65536
 MAX_LOSS_ROWS = 1 << 20
-MAX_LOSS_VOCAB = 1 << 24
+MAX_VOCAB = 1 << 24
 
 
 def _own_device(call):
     """Runs the call on its first argument's device (its current stream), whichever device is current."""
+    first = next(iter(inspect.signature(call).parameters))
+
     @functools.wraps(call)
-    def on_device(t, *args, **kw):
+    def on_device(*args, **kw):
+        t = args[0] if args else kw.get(first)
         if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != torch.cuda.current_device():
             with torch.cuda.device(t.device):
-                return call(t, *args, **kw)
-        return call(t, *args, **kw)
+                return call(*args, **kw)
+        return call(*args, **kw)
     return on_device
 
 
@@ -803,6 +807,8 @@ def _rows_like(lead, cols: int, dtype, device) -> torch.Tensor:
     step = _STEP[dtype]
     if cols % step == 0:
         return torch.empty((*lead, cols), dtype=dtype, device=device)
+    if len(lead) == 1:
+        return torch.empty_strided((lead[0], cols), (-(-cols // step) * step, 1), dtype=dtype, device=device)
     strides = [1, -(-cols // step) * step]
     for n in reversed(lead[1:]):
         strides.append(strides[-1] * n)
@@ -880,11 +886,19 @@ def rmsnorm_quant(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residu
         rs = _matrix(residual, "residual", x.dtype, dev, D)[2]
     if weight is not None:
         _vector(weight, "weight", x.dtype, dev, D)
-    if out is None and D % 16 == 0 and x.is_contiguous():  # the ordinary call: nothing to look at in the outputs
-        q, scale = torch.empty_like(x, dtype=torch.int8), x.new_empty(rows, dtype=torch.float32)
-        h = None if residual is None else torch.empty_like(x)
-        y = torch.empty_like(x, dtype=torch.bfloat16) if want_values else None
-        qs = hs = vs = D
+    if out is None:  # the ordinary call: nothing to look at in the outputs
+        scale = x.new_empty(rows, dtype=torch.float32)
+        if D % 16 == 0 and x.is_contiguous():
+            q = torch.empty_like(x, dtype=torch.int8)
+            h = None if residual is None else torch.empty_like(x)
+            y = torch.empty_like(x, dtype=torch.bfloat16) if want_values else None
+            qs = hs = vs = D
+        else:
+            lead, device, step = shape[:-1], x.device, _STEP[x.dtype]
+            q = _rows_like(lead, D, torch.int8, device)
+            h = None if residual is None else _rows_like(lead, D, x.dtype, device)
+            y = _rows_like(lead, D, torch.bfloat16, device) if want_values else None
+            qs, hs, vs = -(-D // 16) * 16, -(-D // step) * step, -(-D // 8) * 8
         o = {"q": q, "scale": scale}
         if h is not None:
             o["residual"] = h

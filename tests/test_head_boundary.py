@@ -1,5 +1,5 @@
 """The output head's C-ABI calls and binding without a GPU: bad arguments are refused on the host, before any launch."""
-import ctypes
+import os
 
 import pytest
 import torch
@@ -57,6 +57,7 @@ def test_head_limits(tslt):
     assert head(tslt, dtype=2) == tslt.ERR_UNSUPPORTED
     assert head(tslt, D=65537, qst=65552, wst=65552) == tslt.ERR_UNSUPPORTED
     assert head(tslt, n=128) == tslt.ERR_WORKSPACE
+    assert head(tslt, rows=(1 << 24) + 1) == tslt.ERR_UNSUPPORTED and head(tslt, V=(1 << 24) + 1, zst=1 << 25) == tslt.ERR_UNSUPPORTED
     assert head(tslt, rows=0, q=None, z=None) == tslt.OK
 
 
@@ -67,7 +68,7 @@ def fwd(lib, **k):
 
 
 def bwd(lib, **k):
-    a = dict(h=P, hst=64, w=P, wst=64, t=P, lse=P, dl=None, rows=5, V=100, D=64, dh=P, dhst=64, dw=P, dwst=64, wsp=WS, n=1 << 40)
+    a = dict(h=P, hst=64, w=2 * P, wst=64, t=P, lse=P, dl=None, rows=5, V=100, D=64, dh=3 * P, dhst=64, dw=4 * P, dwst=64, wsp=WS, n=1 << 40)
     a.update(k)
     return lib.lib().tslt_linear_ce_backward(*[a[n] for n in ("h", "hst", "w", "wst", "t", "lse", "dl", "rows", "V", "D", "dh", "dhst", "dw",
                                                             "dwst", "wsp", "n")], None)
@@ -82,7 +83,8 @@ def test_loss_refuses(tslt, bad):
     assert fwd(tslt, **bad) == tslt.ERR_INVALID_ARG
 
 
-@pytest.mark.parametrize("bad", COMMON + [dict(dh=None), dict(dh=P + 8), dict(dhst=60), dict(dw=None), dict(dwst=68)])
+@pytest.mark.parametrize("bad", COMMON + [dict(dh=None), dict(dh=P + 8), dict(dhst=60), dict(dw=None), dict(dwst=68), dict(dh=P), dict(dw=2 * P),
+                                          dict(dw=3 * P), dict(dw=P)])
 def test_loss_backward_refuses(tslt, bad):
     assert bwd(tslt, **bad) == tslt.ERR_INVALID_ARG
 
@@ -113,8 +115,17 @@ def test_binding_refuses_cpu_tensors(tslt):
             call()
 
 
-def test_no_call_keeps_its_arguments(tslt):
-    """The limits that the header states are the binding's."""
-    text = open(__import__("os").path.join(__import__("os").path.dirname(__import__("os").path.dirname(__file__)), "include", "tslt.h")).read()
+def test_keyword_arguments(tslt):
+    """Every argument can be given by its name, the first one too."""
+    x = torch.zeros(2, 64)
+    with pytest.raises(ValueError, match="CUDA"):
+        tslt.rmsnorm_quant(x=x, eps=1e-5)
+    with pytest.raises(ValueError, match="CUDA"):
+        tslt.linear_ce(weight=x, target=x, hidden=x)
+
+
+def test_header_and_binding_agree_on_limits(tslt):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "tslt.h")).read()
     assert "#define TSLT_MAX_HIDDEN %d" % tslt.MAX_HIDDEN in text and "#define TSLT_MAX_INT8_K %d" % tslt.MAX_INT8_K in text
-    assert ctypes.sizeof(ctypes.c_longlong) == 8
+    assert "#define TSLT_MAX_LOSS_ROWS (1 << %d)" % (tslt.MAX_LOSS_ROWS.bit_length() - 1) in text
+    assert "#define TSLT_MAX_VOCAB (1 << %d)" % (tslt.MAX_VOCAB.bit_length() - 1) in text
