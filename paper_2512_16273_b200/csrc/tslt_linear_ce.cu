@@ -337,8 +337,10 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and t
                 asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[j]) : "f"(hi), "f"(lo));
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                reinterpret_cast<uint4*>(at(c))[j] = make_uint4(b[4 * j], b[4 * j + 1], b[4 * j + 2], b[4 * j + 3]);
+            for (int j = 0; j < 2; ++j)  // whole sectors
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at(c) + 16 * j), "r"(b[8 * j]), "r"(b[8 * j + 1]),
+                             "r"(b[8 * j + 2]), "r"(b[8 * j + 3]), "r"(b[8 * j + 4]), "r"(b[8 * j + 5]), "r"(b[8 * j + 6]), "r"(b[8 * j + 7])
+                             : "memory");
         }
         // the target's entry, by the part that wrote its column
         const bool here = col >= 0 && col < n && (col / 32) % kParts == part;
