@@ -153,6 +153,19 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
         s_before = s_all = 0;
         s_top = 0u;
     }
+    // the loads of a warp's first row are in flight while the targets are counted (an ignored row's are thrown away)
+    const int vecs = (int)(p.s.ds / 8), row1 = first + warp;
+    const int t1 = row1 < last ? __ldg(p.target + row1) : -1;
+    uint4 v[4], u[4];
+    auto load = [&](const uint16_t* h, const uint16_t* w, int i0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = row_vec(h, i0 + 32 * k, p.D);
+        if (p.loss) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = row_vec(w, i0 + 32 * k, p.D);
+        }
+    };
+    if (counts(t1, p.V)) load(p.hidden + row1 * p.h_stride, p.weight + t1 * p.w_stride, lane);
     __syncthreads();
     int before = 0, all = 0, bad = 0;
     float top = 0.f;
@@ -181,7 +194,6 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
         *p.s.count = s_all;
         *p.s.top_weight = wtop;
     }
-    const int vecs = (int)(p.s.ds / 8);
     int at0 = s_before;
     for (int r0 = first; r0 < last; r0 += 32) {  // 32 rows: a ballot gives each its place
         const int mine = r0 + lane < last ? __ldg(p.target + r0 + lane) : -1;
@@ -194,13 +206,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
                 uint4* dst = reinterpret_cast<uint4*>(p.s.hidden) + (size_t)at * 8;
                 float z = 0.f;
                 for (int i0 = lane; i0 < vecs; i0 += 128) {  // four (eight with the weight's row) loads in flight
-                    uint4 v[4], u[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = row_vec(h, i0 + 32 * k, p.D);
-                    if (p.loss) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) u[k] = row_vec(w, i0 + 32 * k, p.D);
-                    }
+                    if (row != row1 || i0 != lane) load(h, w, i0);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int i = i0 + 32 * k;
@@ -452,28 +458,42 @@ __global__ void __launch_bounds__(32 * kJoinWarps) ce_join_kernel(CeSpace s, int
     const int row = blockIdx.x * 32 + lane, rows = *s.count;
     if ((int)blockIdx.x * 32 >= rows) return;
     const float2* at = s.part + (row < rows ? row : 0);
+    const int src = row < rows ? s.row_of[row] : 0;
+    const float zt = row < rows ? s.ztarget[row] : 0.f;
     float m = -INFINITY;
-#pragma unroll 8
-    for (int t = warp; t < parts; t += kJoinWarps) m = fmaxf(m, at[t * s.rows_pad].x);
-    s_m[warp][lane] = m;
-    __syncthreads();
-    m = s_m[0][lane];
-    for (int w = 1; w < kJoinWarps; ++w) m = fmaxf(m, s_m[w][lane]);
     double sum = 0.0;
-#pragma unroll 8
-    for (int t = warp; t < parts; t += kJoinWarps) {
-        const float2 v = at[t * s.rows_pad];
-        sum += (double)(v.y * ex2_approx(v.x - m));
+    for (int t0 = warp; t0 < parts; t0 += 8 * kJoinWarps) {  // eight pairs in flight
+        float2 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int t = t0 + j * kJoinWarps;
+            v[j] = t < parts ? at[t * s.rows_pad] : make_float2(-INFINITY, 0.f);
+        }
+        float top = v[0].x;
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, v[j].x);
+        if (top > m) {
+            sum *= (double)ex2_approx(m - top);
+            m = top;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            sum += (double)(v[j].y * ex2_approx(v[j].x - (m == -INFINITY ? 0.f : m)));  // (a part without columns: -inf and 0)
     }
+    s_m[warp][lane] = m;
     s_s[warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && row < rows) {
+        float top = s_m[0][lane];
+#pragma unroll
+        for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, s_m[w][lane]);
         double all = 0.0;
-        for (int w = 0; w < kJoinWarps; ++w) all += s_s[w][lane];
-        const double l = kLn2 * ((double)m + log2(all));
-        const int src = s.row_of[row];
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w)
+            if (s_s[w][lane] != 0.0) all += s_s[w][lane] * (double)ex2_approx(s_m[w][lane] - top);  // (a warp without tiles has -inf and 0)
+        const double l = kLn2 * ((double)top + log2(all));
         lse[src] = (float)l;
-        loss[src] = (float)(l - (double)s.ztarget[row]);
+        loss[src] = (float)(l - (double)zt);
     }
 }
 
@@ -485,6 +505,7 @@ __global__ void __launch_bounds__(256 * kGroups) ce_scatter_kernel(CeSpace s, ui
     __shared__ float4 sums[kGroups > 1 ? kGroups - 1 : 1][16][32];
     __shared__ uint32_t tile[32][33];
     wait_for_primary_kernel();
+    allow_dependent_launch();
     const int rows = *s.count, r0 = blockIdx.x * 32, d0 = blockIdx.y * 64;
     if (r0 >= rows) return;
     const float scale = *s.top_weight;
@@ -694,6 +715,13 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         const HiddenEpilogue::Params eh = {(float4*)s.acc, s.rows_pad, s.da, D, c == 0};
         if (const int rc = product<HiddenEpilogue, 4>(s.pair, ta, tb, p, eh, st)) return rc;
 
+        if (c == s.pieces - 1) {  // dH is whole, and its sums still in L2
+            const dim3 grid((rows + 31) / 32, (D + 63) / 64);
+            if (const int rc = s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
+                                             : launch_after(ce_scatter_kernel<1>, grid, 256, st, s, (uint16_t*)dhidden, dhidden_stride, D))
+                return rc;
+        }
+
         // dW of the piece: rows are vocabulary entries, the sum runs over the rows that count
         p.m_tiles = (int)(up(width, tile_rows) / tile_rows);
         p.k_blocks = (int)(s.rows_pad / 64);
@@ -710,7 +738,5 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
         if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
     }
-    const dim3 grid((rows + 31) / 32, (D + 63) / 64);
-    return s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
-                         : launch_after(ce_scatter_kernel<1>, grid, 256, st, s, (uint16_t*)dhidden, dhidden_stride, D);
+    return TSLT_OK;
 }
