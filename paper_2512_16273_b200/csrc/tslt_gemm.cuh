@@ -16,12 +16,17 @@
 // DRAM pages and full lines, whichever way it is read).  Out-of-range rows and columns of a copy read as zero, so that
 // ragged sizes need no special case before the epilogue.
 //
+// Two products.  A kernel can carry a second product of the same tile width: its tiles follow the first's on every cluster,
+// so that neither's last round leaves the machine idle and a product bound by memory runs beside one bound by arithmetic.
+//
 // Waits.  Every wait on a barrier is bounded (kWaitLimit polls).  One that runs out sets an abort flag in shared memory
 // and TSLT_STATUS_WAIT_TIMEOUT in the status word; every role then leaves its loop, copies in flight are waited for
 // (bounded as well), tensor memory is freed and the kernel returns.
 #pragma once
 
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "tslt_common.cuh"
 
@@ -256,8 +261,8 @@ struct Waiter {
     }
 };
 
-// The tiles of one cluster: every role of both CTAs walks the same list.  Order: groups of group_m row tiles, all
-// column tiles of a group before the next group, row tiles fastest (the rows of a group stay in L2 while B streams).
+// The tiles of a product: every role of both CTAs decodes the same list.  Order: groups of group_m row tiles, all column tiles
+// of a group before the next group, row tiles fastest (the rows of a group stay in L2 while B streams).
 struct Walk {
     int m_tiles, per_split, total, rows, k_blocks;
     __device__ __forceinline__ Walk(const Product& p, int tile_rows) {
@@ -287,10 +292,45 @@ struct Walk {
     }
 };
 
-template <bool kInt8, int kCtas, int kEpiWarps, class Epi>
+// Which tiles a cluster takes.  The first product's in turn: q or q + 1 of them, the first r clusters one more.  Then the second's:
+// the clusters that had one less take `ahead` of its tiles before the others join, as many as that one tile was worth.
+struct Plan {
+    int clusters, cluster, total1, total2, mine1, fewer, ahead;
+    __device__ __forceinline__ Plan(int cluster_, int clusters_, int total1_, int total2_, int cost1, int cost2)
+        : clusters(clusters_), cluster(cluster_), total1(total1_), total2(total2_) {
+        const int r = total1 % clusters;
+        mine1 = total1 / clusters + (cluster < r);
+        fewer = clusters - r;  // clusters with one tile less (all of them when r = 0)
+        ahead = r ? (cost1 + cost2 / 2) / cost2 : 0;
+    }
+    // the i-th tile of this cluster: its number in its product, or -1 behind the last
+    __device__ __forceinline__ int at(int i, bool* second) const {
+        *second = i >= mine1;
+        if (i < mine1) return cluster + i * clusters;
+        i -= mine1;
+        const int first = clusters - fewer;
+        int n;
+        if (cluster >= first && i < ahead) n = i * fewer + cluster - first;
+        else n = ahead * fewer + (cluster >= first ? i - ahead : i) * clusters + cluster;
+        return n < total2 ? n : -1;
+    }
+};
+
+struct Maps {
+    CUtensorMap a, b;
+};
+struct NoEpilogue {
+    static constexpr bool kOutBox = false;
+    struct Params {};
+};
+// A tile whose sum is short costs its epilogue: about ten stages.
+__device__ __forceinline__ int tile_cost(int k_blocks) { return k_blocks > 10 ? k_blocks : 10; }
+
+template <bool kInt8, int kCtas, int kEpiWarps, class Epi, class Epi2>
 __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
-    gemm_kernel(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensorMap tb, const __grid_constant__ Product p,
-                const __grid_constant__ typename Epi::Params ep) {
+    gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Product p, const __grid_constant__ typename Epi::Params ep,
+                const __grid_constant__ Maps maps2, const __grid_constant__ Product p2, const __grid_constant__ typename Epi2::Params ep2) {
+    constexpr bool kDual = !std::is_same<Epi2, NoEpilogue>::value;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
     uint8_t* const basep = smem_raw + (base - smem_u32(smem_raw));
@@ -316,8 +356,8 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
         mbar_init(drain, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&ta) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&tb) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
     }
     if (warp == 1) tmem_alloc<kCtas>(tmem_slot);
     tc_fence_before();
@@ -329,16 +369,22 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
     allow_dependent_launch();
     if (p.clear_status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
     const Waiter wait = {abort_flag, p.status};
-    const Walk walk(p, kTileRows);
+    const Walk walk(p, kTileRows), walk2(kDual ? p2 : p, kTileRows);
+    const Plan plan(cluster, clusters, walk.total, kDual ? walk2.total : 0, tile_cost(walk.k_blocks / p.splits), tile_cost(walk2.k_blocks));
+    bool second;
 
     if (warp == 0) {
         if (lane == 0) {
             const uint32_t tx = (uint32_t)stage_bytes * kCtas;
             int stage = 0, phase = 0;
             bool ok = true;
-            for (int idx = cluster; idx < walk.total && ok; idx += clusters) {
-                const Tile t = walk.at(p, idx, kTileRows, rank);
+            for (int i = 0, idx; ok && (idx = plan.at(i, &second)) >= 0; ++i) {
+                const bool two = kDual && second;
+                const Tile t = two ? walk2.at(p2, idx, kTileRows, rank) : walk.at(p, idx, kTileRows, rank);
                 const int brow = t.col0 + rank * (p.nt / kCtas);
+                const int a_layout = two ? p2.a_layout : p.a_layout, b_layout = two ? p2.b_layout : p.b_layout;
+                const int pitch = two ? p2.pitch : p.pitch, k_elems = two ? p2.k_elems : p.k_elems;
+                const CUtensorMap *ta = two ? &maps2.a : &maps.a, *tb = two ? &maps2.b : &maps.b;
                 for (int kb = t.k_begin; kb < t.k_end; ++kb) {
                     if (!wait(empty + 8 * stage, phase ^ 1)) {
                         ok = false;
@@ -348,9 +394,9 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
                     uint32_t bar = full + 8 * stage;
                     if (rank == 0) mbar_expect(bar, tx);
                     if (kCtas == 2) bar = map_to_rank(bar, 0);
-                    const int k0 = kb * p.k_elems;
-                    load_operand<kCtas>(sa, &ta, p.a_layout, p.pitch, t.row0, 128, k0, bar);
-                    load_operand<kCtas>(sb, &tb, p.b_layout, p.pitch, brow, p.nt / kCtas, k0, bar);
+                    const int k0 = kb * k_elems;
+                    load_operand<kCtas>(sa, ta, a_layout, pitch, t.row0, 128, k0, bar);
+                    load_operand<kCtas>(sb, tb, b_layout, pitch, brow, p.nt / kCtas, k0, bar);
                     if (++stage == p.stages) {
                         stage = 0;
                         phase ^= 1;
@@ -375,10 +421,12 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
         if (lane == 0 && rank == 0) {
             int stage = 0, phase = 0, acc = 0, acc_phase = 0;
             bool ok = true;
-            const bool a_mn = p.a_layout >= kBlocksMN, b_mn = p.b_layout >= kBlocksMN;
-            const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
-            for (int idx = cluster; idx < walk.total && ok; idx += clusters) {
-                const Tile t = walk.at(p, idx, kTileRows, rank);
+            for (int i = 0, idx; ok && (idx = plan.at(i, &second)) >= 0; ++i) {
+                const bool two = kDual && second;
+                const Tile t = two ? walk2.at(p2, idx, kTileRows, rank) : walk.at(p, idx, kTileRows, rank);
+                const bool a_mn = (two ? p2.a_layout : p.a_layout) >= kBlocksMN, b_mn = (two ? p2.b_layout : p.b_layout) >= kBlocksMN;
+                const uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;
+                const uint32_t idesc = two ? p2.idesc : p.idesc;
                 if (t.k_begin >= t.k_end) continue;  // nothing to add up: the epilogue takes zeros
                 if (!wait(tempty + 8 * acc, acc_phase ^ 1)) break;
                 tc_fence_after();
@@ -393,7 +441,7 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
                     const uint64_t da = make_desc(sa, a_mn ? 8192 : 16), db = make_desc(sa + kStageA, b_mn ? 8192 : 16);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        mma<kCtas, kInt8>(d, da + j * a_step, db + j * b_step, p.idesc, kb > t.k_begin || j > 0);
+                        mma<kCtas, kInt8>(d, da + j * a_step, db + j * b_step, idesc, kb > t.k_begin || j > 0);
                     mma_commit<kCtas>(empty + 8 * stage);
                     if (++stage == p.stages) {
                         stage = 0;
@@ -415,16 +463,23 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
         const uint32_t out = data + p.stages * stage_bytes;
         WarpSmem own = {out + (warp - 2) * 2 * kStageOut, out + kEpiWarps * 2 * kStageOut + (warp - 2) * kScratch, 0};
         int acc = 0, acc_phase = 0;
-        for (int idx = cluster; idx < walk.total; idx += clusters) {
-            const Tile t = walk.at(p, idx, kTileRows, rank);
+        for (int i = 0, idx; (idx = plan.at(i, &second)) >= 0; ++i) {
+            const bool two = kDual && second;
+            const Tile t = two ? walk2.at(p2, idx, kTileRows, rank) : walk.at(p, idx, kTileRows, rank);
             const bool empty_sum = t.k_begin >= t.k_end;
             if (!empty_sum) {
                 const bool got = wait(tfull + 8 * acc, acc_phase);
                 if (!__all_sync(0xffffffffu, got)) break;
                 tc_fence_after();
             }
-            Epi::template run<kEpiWarps / 4>(ep, tmem + ((uint32_t)(quad * 32) << 16) + acc * kAccCols, empty_sum, t, t.row0 + quad * 32 + lane,
-                                             lane, part, own);
+            const uint32_t sums = tmem + ((uint32_t)(quad * 32) << 16) + acc * kAccCols;
+            const int row = t.row0 + quad * 32 + lane;
+            if constexpr (kDual) {
+                if (two) Epi2::template run<kEpiWarps / 4>(ep2, sums, empty_sum, t, row, lane, part, own);
+                else Epi::template run<kEpiWarps / 4>(ep, sums, empty_sum, t, row, lane, part, own);
+            } else {
+                Epi::template run<kEpiWarps / 4>(ep, sums, empty_sum, t, row, lane, part, own);
+            }
             if (!empty_sum) {
                 tc_fence_before();
                 __syncwarp();
@@ -434,7 +489,7 @@ __global__ void __launch_bounds__(64 + 32 * kEpiWarps, 1)
             }
         }
     }
-    if (Epi::kOutBox && warp >= 2 && lane == 0) store_wait_all();
+    if ((Epi::kOutBox || Epi2::kOutBox) && warp >= 2 && lane == 0) store_wait_all();
     __syncwarp();
     tc_fence_before();
     if (kCtas == 2) cluster_sync();
@@ -471,15 +526,18 @@ inline uint32_t instruction_desc(bool int8, int m, int n, bool a_mn, bool b_mn) 
 
 // Fills idesc and stages from nt, launches on min(tiles, SMs) clusters.  dependent: the kernel before it on the stream is
 // this call's own and its results are waited for inside (programmatic launch).
-template <bool kInt8, int kCtas, int kEpiWarps, class Epi>
-int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typename Epi::Params& ep, bool dependent, cudaStream_t st) {
+template <bool kInt8, int kCtas, int kEpiWarps, class Epi, class Epi2>
+int launch_two(const Maps& maps, Product p, const typename Epi::Params& ep, const Maps& maps2, Product p2, const typename Epi2::Params& ep2,
+               bool dependent, cudaStream_t st) {
+    constexpr bool kDual = !std::is_same<Epi2, NoEpilogue>::value;
     const int sms = sm_count();
     if (sms <= 0) return TSLT_ERR_CUDA;
-    const int stage = kStageA + p.nt / kCtas * 128, boxes = Epi::kOutBox ? kEpiWarps * (2 * kStageOut + kScratch) : 0;
+    const int stage = kStageA + p.nt / kCtas * 128, boxes = Epi::kOutBox || Epi2::kOutBox ? kEpiWarps * (2 * kStageOut + kScratch) : 0;
     p.stages = (kSmemLimit - 1024 - kBarrierBytes - boxes) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.idesc = instruction_desc(kInt8, 128 * kCtas, p.nt, p.a_layout >= kBlocksMN, p.b_layout >= kBlocksMN);
-    auto kern = gemm_kernel<kInt8, kCtas, kEpiWarps, Epi>;
+    p2.idesc = instruction_desc(kInt8, 128 * kCtas, p.nt, p2.a_layout >= kBlocksMN, p2.b_layout >= kBlocksMN);
+    auto kern = gemm_kernel<kInt8, kCtas, kEpiWarps, Epi, Epi2>;
     const int smem = 1024 + kBarrierBytes + p.stages * stage + boxes;
     static bool done[64] = {};
     int dev = -1;
@@ -488,10 +546,10 @@ int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typena
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess) return TSLT_ERR_CUDA;
         if (dev >= 0 && dev < 64) done[dev] = true;
     }
-    const long long tiles = (long long)p.m_tiles * p.n_tiles * p.splits;
-    if (tiles <= 0) return TSLT_OK;
-    if (tiles > 0x7fffffffLL) return TSLT_ERR_UNSUPPORTED;
-    const long long clusters = tiles < sms / kCtas ? tiles : sms / kCtas;
+    const long long tiles = (long long)p.m_tiles * p.n_tiles * p.splits, tiles2 = kDual ? (long long)p2.m_tiles * p2.n_tiles * p2.splits : 0;
+    if (tiles + tiles2 <= 0) return TSLT_OK;
+    if (tiles > 0x3fffffffLL || tiles2 > 0x3fffffffLL) return TSLT_ERR_UNSUPPORTED;
+    const long long clusters = tiles + tiles2 < sms / kCtas ? tiles + tiles2 : sms / kCtas;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * kCtas), 1, 1);
     cfg.blockDim = dim3(64 + 32 * kEpiWarps, 1, 1);
@@ -506,7 +564,11 @@ int launch(const CUtensorMap& ta, const CUtensorMap& tb, Product p, const typena
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kCtas > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, ta, tb, p, ep) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kern, maps, p, ep, maps2, p2, ep2) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+}
+template <bool kInt8, int kCtas, int kEpiWarps, class Epi>
+int launch(const Maps& maps, const Product& p, const typename Epi::Params& ep, bool dependent, cudaStream_t st) {
+    return launch_two<kInt8, kCtas, kEpiWarps, Epi, NoEpilogue>(maps, p, ep, maps, p, NoEpilogue::Params{}, dependent, st);
 }
 
 // The column width of a tile, a multiple of `unit`, at most 256: the one whose rounds of tiles over the machine's clusters cost

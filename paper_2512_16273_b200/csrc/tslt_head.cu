@@ -236,7 +236,7 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
     p.k_blocks = (K + 127) / 128;
     p.status = status;
     p.clear_status = 1;
-    CUtensorMap ta, tb;
+    gemm::Maps maps;
     if (rows >= kManyRows) {
         p.m_tiles = (rows + 255) / 256;
         p.nt = gemm::choose_nt(p.m_tiles, V, true, HeadRowsEpilogue<T>::kCols);
@@ -245,20 +245,20 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
         p.m_total = rows;
         typename HeadRowsEpilogue<T>::Params ep = {{}, out, out_stride, qs, ws, rows, V};
         const int step = 16 / sizeof(T);
-        if (!gemm::encode_map(&ta, gemm::kElemInt8, q, K, rows, q_stride, 128) || !gemm::encode_map(&tb, gemm::kElemInt8, w, K, V, w_stride, p.nt / 2) ||
+        if (!gemm::encode_map(&maps.a, gemm::kElemInt8, q, K, rows, q_stride, 128) || !gemm::encode_map(&maps.b, gemm::kElemInt8, w, K, V, w_stride, p.nt / 2) ||
             !gemm::encode_map(&ep.out, sizeof(T) == 4 ? gemm::kElemFp32 : gemm::kElemBf16, out, V < step ? step : V / step * step, rows,
                               out_stride * (long long)sizeof(T), 32))
             return TSLT_ERR_CUDA;
-        return gemm::launch<true, 2, 4, HeadRowsEpilogue<T>>(ta, tb, p, ep, false, st);
+        return gemm::launch<true, 2, 4, HeadRowsEpilogue<T>>(maps, p, ep, false, st);
     }
     p.nt = rows <= 16 ? 16 : (rows + 31) / 32 * 32;
     p.n_tiles = 1;
     p.m_tiles = (V + 127) / 128;
     p.group_m = 1;
     p.m_total = V;
-    if (!gemm::encode_map(&ta, gemm::kElemInt8, w, K, V, w_stride, 128) || !gemm::encode_map(&tb, gemm::kElemInt8, q, K, rows, q_stride, p.nt)) return TSLT_ERR_CUDA;
+    if (!gemm::encode_map(&maps.a, gemm::kElemInt8, w, K, V, w_stride, 128) || !gemm::encode_map(&maps.b, gemm::kElemInt8, q, K, rows, q_stride, p.nt)) return TSLT_ERR_CUDA;
     const typename HeadEpilogue<T>::Params ep = {out, out_stride, qs, ws, rows, V};
-    return gemm::launch<true, 1, 8, HeadEpilogue<T>>(ta, tb, p, ep, false, st);
+    return gemm::launch<true, 1, 8, HeadEpilogue<T>>(maps, p, ep, false, st);
 }
 
 }  // namespace tslt

@@ -60,25 +60,16 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     s.pieces = (int)((vt + c - 1) / c);
     s.piece = up((vt + s.pieces - 1) / s.pieces, kTileN);
     s.pieces = (int)((vt + s.piece - 1) / s.piece);
-    // dH: cut its sum over the piece so that the last round of tiles wastes little.  How many rows count is only known on
-    // the device: the rule averages over all of them and three quarters, and charges each buffer what adding to it costs
-    // next to a piece's products (3.4 % at 16128 entries, measured; it goes with 1 / piece).  Few rows have few tiles and
-    // a long sum: there, as many cuts as fill the machine.
+    // dH's tiles come first on their clusters and dW's fill up behind them (one kernel), so a tile of dH may be as long as a
+    // cluster's whole share of both: cut its sum over the piece where it is longer (few rows: few tiles, a long sum).
+    // Sums in stages; a tile of dW costs its epilogue, ten stages, where its own sum is shorter.
     const long long tile_rows = s.pair ? 256 : 128, slots = s.pair ? 74 : 148, cols = up(D, kTileN) / kTileN;
-    const long long m_all = up(rows, tile_rows) / tile_rows, m_less = up((rows * 3ll + 3) / 4, tile_rows) / tile_rows;
-    auto waste = [&](long long tiles, long long cuts) { return (double)(up(tiles * cuts, slots)) / (double)(tiles * cuts); };
-    long long most = slots / (m_all * cols);
-    if (most < 8) most = 8;
-    if (most > s.piece / 512) most = s.piece / 512;  // 8 stages a cut at least
-    s.splits = 1;
-    double best = 1e30;
-    for (long long c = 1; c <= most; ++c) {
-        const double cost = (waste(m_all * cols, c) + waste(m_less * cols, c)) * 0.5 + (s.pieces > 1 ? 550.0 : 275.0) / (double)s.piece * (double)c;
-        if (cost < best) {
-            best = cost;
-            s.splits = (int)c;
-        }
-    }
+    const long long k1 = s.piece / 64, k2 = s.rows_pad / 64 < 10 ? 10 : s.rows_pad / 64;
+    const long long tiles1 = up(rows, tile_rows) / tile_rows * cols, share = (tiles1 * k1 + up(s.piece, tile_rows) / tile_rows * cols * k2) / slots;
+    const long long most1 = s.pair ? share : share / 4;  // few rows: four tiles of dH to a share, their sums are small (77 rows: 101 us, one: 118)
+    s.splits = (int)(most1 < 1 ? k1 : (k1 + most1 - 1) / most1);
+    if (s.splits > k1 / 8) s.splits = (int)(k1 / 8);  // eight stages a cut at least
+    if (s.splits < 1) s.splits = 1;
     uint8_t* p = (uint8_t*)ws;
     size_t at = kWsHeaderBytes;
     auto take = [&](size_t n) {
@@ -587,15 +578,15 @@ static int launch_after(void (*kernel)(Args...), dim3 grid, int threads, cudaStr
 }
 
 template <class Epi, int kWarps>
-static int product(bool pair, const CUtensorMap& ta, const CUtensorMap& tb, const gemm::Product& p, const typename Epi::Params& ep, cudaStream_t st) {
-    return pair ? gemm::launch<false, 2, kWarps, Epi>(ta, tb, p, ep, true, st) : gemm::launch<false, 1, kWarps, Epi>(ta, tb, p, ep, true, st);
+static int product(bool pair, const gemm::Maps& maps, const gemm::Product& p, const typename Epi::Params& ep, cudaStream_t st) {
+    return pair ? gemm::launch<false, 2, kWarps, Epi>(maps, p, ep, true, st) : gemm::launch<false, 1, kWarps, Epi>(maps, p, ep, true, st);
 }
 
 // z of `width` vocabulary entries of the weight, in tiles that reach column `cover` at least: the product that forward and
 // backward share.
 static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, long long w_stride, long long width, long long cover, int nt,
                           gemm::Product* p,
-                          CUtensorMap* ta, CUtensorMap* tb) {
+                          gemm::Maps* maps) {
     *p = gemm::Product{};
     const int tile_rows = s.pair ? 256 : 128;
     p->m_tiles = (int)(up(rows, tile_rows) / tile_rows);
@@ -610,8 +601,8 @@ static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, 
     p->status = s.status;
     p->a_layout = gemm::kPanelsK;
     p->pitch = (int)s.rows_pad;
-    return gemm::encode_map(ta, gemm::kElemBf16, s.hidden, 64, s.ds / 64 * s.rows_pad, 128, 128) &&
-                   gemm::encode_map(tb, gemm::kElemBf16, w, D, width, w_stride * 2, s.pair ? nt / 2 : nt)
+    return gemm::encode_map(&maps->a, gemm::kElemBf16, s.hidden, 64, s.ds / 64 * s.rows_pad, 128, 128) &&
+                   gemm::encode_map(&maps->b, gemm::kElemBf16, w, D, width, w_stride * 2, s.pair ? nt / 2 : nt)
                ? TSLT_OK
                : TSLT_ERR_CUDA;
 }
@@ -658,13 +649,13 @@ extern "C" int tslt_linear_ce(const void* hidden, long long hidden_stride, const
     if (workspace_bytes < s.bytes) return TSLT_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)stream;
     gemm::Product p;
-    CUtensorMap ta, tb;
-    if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, V, s.nt, &p, &ta, &tb)) return rc;
+    gemm::Maps maps;
+    if (const int rc = logits_product(s, rows, D, (const uint16_t*)weight, weight_stride, V, V, s.nt, &p, &maps)) return rc;
     const GatherParams g = {(const uint16_t*)hidden, (const uint16_t*)weight, target, hidden_stride, weight_stride, rows, V, D, 0, nullptr,
                             nullptr, loss, lse, nullptr, 0, s};
     if (const int rc = gather(g, st)) return rc;
     const StatsEpilogue::Params ep = {log2e_for(D), s.part, s.ztarget, s.target, s.rows_pad, V};
-    if (const int rc = product<StatsEpilogue, 4 * kStatsParts>(s.pair, ta, tb, p, ep, st)) return rc;
+    if (const int rc = product<StatsEpilogue, 4 * kStatsParts>(s.pair, maps, p, ep, st)) return rc;
     return launch_after(ce_join_kernel, dim3((rows + 31) / 32), 32 * kJoinWarps, st, s, (int)s.tiles * kStatsParts, loss, lse);
 }
 
@@ -691,14 +682,14 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
     for (int c = 0; c < s.pieces; ++c) {
         const long long v0 = c * s.piece, width = v0 + s.piece < V ? s.piece : V - v0;
         gemm::Product p;
-        CUtensorMap ta, tb;
+        gemm::Maps maps;
         if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width, up(width, 64),  // dH sums in steps of 64
-                                         gemm::choose_nt((rows + tile_rows - 1) / tile_rows, width, s.pair != 0, 32), &p, &ta, &tb)) return rc;
+                                         gemm::choose_nt((rows + tile_rows - 1) / tile_rows, width, s.pair != 0, 32), &p, &maps)) return rc;
         const GradEpilogue::Params eg = {log2e_for(D), s.g, s.lse2, s.weight, s.target, s.rows_pad, (int)v0, (int)width};
-        if (const int rc = product<GradEpilogue, 8>(s.pair, ta, tb, p, eg, st)) return rc;
+        if (const int rc = product<GradEpilogue, 8>(s.pair, maps, p, eg, st)) return rc;
 
-        // the piece's part of dH first, while the weight's piece is still in L2 from the product above: the sum runs over the
-        // piece's vocabulary entries
+        // one kernel for both products that read G.  The piece's part of dH first, while the weight's piece is still in L2 from
+        // the product above: its sum runs over the piece's vocabulary entries
         const int ctas = s.pair ? 2 : 1, b_blocks = nt / ctas / 64;
         const uint16_t* wp = w + v0 * weight_stride;
         p.m_tiles = (int)(up(rows, tile_rows) / tile_rows);
@@ -708,35 +699,33 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         p.splits = s.splits;
         p.group_m = 8;
         p.b_layout = D % 64 == 0 ? gemm::kBlocksMN : gemm::kRowsMN;
-        if (!gemm::encode_map(&ta, gemm::kElemBf16, s.g, 64, s.piece / 64 * s.rows_pad, 128, 128) ||
-            !(D % 64 == 0 ? gemm::encode_blocks(&tb, wp, width, weight_stride * 2, D / 64, 128, b_blocks)
-                          : gemm::encode_map(&tb, gemm::kElemBf16, wp, D, width, weight_stride * 2, 64)))
+        if (!gemm::encode_map(&maps.a, gemm::kElemBf16, s.g, 64, s.piece / 64 * s.rows_pad, 128, 128) ||
+            !(D % 64 == 0 ? gemm::encode_blocks(&maps.b, wp, width, weight_stride * 2, D / 64, 128, b_blocks)
+                          : gemm::encode_map(&maps.b, gemm::kElemBf16, wp, D, width, weight_stride * 2, 64)))
             return TSLT_ERR_CUDA;
         const HiddenEpilogue::Params eh = {(float4*)s.acc, s.rows_pad, s.da, D, c == 0};
-        if (const int rc = product<HiddenEpilogue, 4>(s.pair, ta, tb, p, eh, st)) return rc;
-
-        if (c == s.pieces - 1) {  // dH is whole, and its sums still in L2
-            const dim3 grid((rows + 31) / 32, (D + 63) / 64);
-            if (const int rc = s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
-                                             : launch_after(ce_scatter_kernel<1>, grid, 256, st, s, (uint16_t*)dhidden, dhidden_stride, D))
-                return rc;
-        }
 
         // dW of the piece: rows are vocabulary entries, the sum runs over the rows that count
-        p.m_tiles = (int)(up(width, tile_rows) / tile_rows);
-        p.k_blocks = (int)(s.rows_pad / 64);
-        p.splits = 1;
-        p.a_layout = p.b_layout = gemm::kBlocksMN;
-        p.m_total = (int)width;
-        p.m_limit = nullptr;
-        p.k_limit = s.count;
-        if (!gemm::encode_blocks(&ta, s.g, s.rows_pad, 128, s.piece / 64, s.rows_pad * 128, 2) ||
-            !gemm::encode_blocks(&tb, s.hidden, s.rows_pad, 128, s.ds / 64, s.rows_pad * 128, b_blocks))
+        gemm::Product p2 = p;
+        gemm::Maps maps2;
+        p2.m_tiles = (int)(up(width, tile_rows) / tile_rows);
+        p2.k_blocks = (int)(s.rows_pad / 64);
+        p2.splits = 1;
+        p2.a_layout = p2.b_layout = gemm::kBlocksMN;
+        p2.m_total = (int)width;
+        p2.m_limit = nullptr;
+        p2.k_limit = s.count;
+        if (!gemm::encode_blocks(&maps2.a, s.g, s.rows_pad, 128, s.piece / 64, s.rows_pad * 128, 2) ||
+            !gemm::encode_blocks(&maps2.b, s.hidden, s.rows_pad, 128, s.ds / 64, s.rows_pad * 128, b_blocks))
             return TSLT_ERR_CUDA;
         uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
         WeightEpilogue::Params ew = {{}, dw, dweight_stride, s.top_weight, (int)width, D};
         if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
-        if (const int rc = product<WeightEpilogue, 4>(s.pair, ta, tb, p, ew, st)) return rc;
+        const int rc = s.pair ? gemm::launch_two<false, 2, 4, HiddenEpilogue, WeightEpilogue>(maps, p, eh, maps2, p2, ew, true, st)
+                              : gemm::launch_two<false, 1, 4, HiddenEpilogue, WeightEpilogue>(maps, p, eh, maps2, p2, ew, true, st);
+        if (rc) return rc;
     }
-    return TSLT_OK;
+    const dim3 grid((rows + 31) / 32, (D + 63) / 64);
+    return s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
+                         : launch_after(ce_scatter_kernel<1>, grid, 256, st, s, (uint16_t*)dhidden, dhidden_stride, D);
 }
