@@ -199,8 +199,9 @@ template <int kCtas> __device__ __forceinline__ void mma_commit(uint32_t bar) {
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 32 columns of this warp's 32 lanes; the values may be used after tmem_wait32().
+// 32 columns of this warp's 32 lanes (all of them take part: they meet first); the values may be used after tmem_wait32().
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
+    __syncwarp();
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -223,6 +224,7 @@ __device__ __forceinline__ void tmem_wait32(uint32_t* r) {
 }
 __device__ __forceinline__ uint32_t tmem_ld1(uint32_t addr) {  // one column, waited for
     uint32_t v;
+    __syncwarp();
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }

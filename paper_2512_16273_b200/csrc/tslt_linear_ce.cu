@@ -43,6 +43,7 @@ struct CeSpace {
     float* acc;        // [splits][da / 4][rows_pad][4]                   (backward)
     long long rows_pad, ds, da, tiles, piece;
     int pieces, splits, pair, nt;  // nt: columns of a tile of z (forward)
+    int direct;                    // one piece and one cut: dH leaves its product as it is wanted
     size_t bytes;
 };
 
@@ -70,6 +71,7 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     s.splits = (int)(most1 < 1 ? k1 : (k1 + most1 - 1) / most1);
     if (s.splits > k1 / 8) s.splits = (int)(k1 / 8);  // eight stages a cut at least
     if (s.splits < 1) s.splits = 1;
+    s.direct = s.pieces == 1 && s.splits == 1;
     uint8_t* p = (uint8_t*)ws;
     size_t at = kWsHeaderBytes;
     auto take = [&](size_t n) {
@@ -87,7 +89,7 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
         s.lse2 = (float*)take(s.rows_pad * 4);
         s.weight = (float*)take(s.rows_pad * 4);
         s.g = (uint16_t*)take(s.rows_pad * s.piece * 2);
-        s.acc = (float*)take((size_t)s.splits * s.rows_pad * s.da * 4);
+        if (!s.direct) s.acc = (float*)take((size_t)s.splits * s.rows_pad * s.da * 4);
     } else {
         s.part = (float2*)take(s.tiles * kStatsParts * s.rows_pad * 8);
         s.ztarget = (float*)take(s.rows_pad * 4);
@@ -438,6 +440,45 @@ struct HiddenEpilogue {  // a piece's part of dH, added up in fp32 (one buffer p
     }
 };
 
+struct HiddenRowsEpilogue {  // dH itself, where one tile sums a row's whole gradient (one piece, one cut): rows to their places
+    static constexpr bool kOutBox = false;
+    struct Params {
+        uint16_t* out;
+        const int* row_of;
+        const float* scale;
+        long long stride;
+        int D, wide;  // wide: rows start on 32-byte boundaries
+    };
+    template <int kParts>
+    static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part, gemm::WarpSmem&) {
+        const bool on = row < t.rows;
+        const float scale = __ldg(p.scale);
+        uint16_t* out = p.out + (on ? __ldg(p.row_of + row) : 0) * p.stride;
+        for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
+            uint32_t r[32], b[16];
+            gemm::tmem_ld32(tmem + c, r);
+            gemm::tmem_wait32(r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b[j]) : "f"(__uint_as_float(r[2 * j + 1]) * scale), "f"(__uint_as_float(r[2 * j]) * scale));
+                if (zero) b[j] = 0;
+            }
+            const int d = t.col0 + c;
+            if (on && p.wide && d + 32 <= p.D) {  // whole sectors
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + d + 16 * j), "r"(b[8 * j]), "r"(b[8 * j + 1]),
+                                 "r"(b[8 * j + 2]), "r"(b[8 * j + 3]), "r"(b[8 * j + 4]), "r"(b[8 * j + 5]), "r"(b[8 * j + 6]), "r"(b[8 * j + 7])
+                                 : "memory");
+            } else if (on) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (d + j < p.D) out[d + j] = (uint16_t)(b[j / 2] >> (16 * (j & 1)));
+            }
+        }
+    }
+};
+
 // ---- small kernels -----------------------------------------------------------------------------------------
 // Joins the tiles' (max, sum) pairs: a CTA takes 32 rows, its warps the tiles in turn; fp64 sums, a fixed order.
 constexpr int kJoinWarps = 32;
@@ -582,6 +623,13 @@ static int product(bool pair, const gemm::Maps& maps, const gemm::Product& p, co
     return pair ? gemm::launch<false, 2, kWarps, Epi>(maps, p, ep, true, st) : gemm::launch<false, 1, kWarps, Epi>(maps, p, ep, true, st);
 }
 
+template <class Epi>
+static int both(bool pair, const gemm::Maps& maps, const gemm::Product& p, const typename Epi::Params& ep, const gemm::Maps& maps2,
+                const gemm::Product& p2, const WeightEpilogue::Params& ep2, cudaStream_t st) {
+    return pair ? gemm::launch_two<false, 2, 4, Epi, WeightEpilogue>(maps, p, ep, maps2, p2, ep2, true, st)
+                : gemm::launch_two<false, 1, 4, Epi, WeightEpilogue>(maps, p, ep, maps2, p2, ep2, true, st);
+}
+
 // z of `width` vocabulary entries of the weight, in tiles that reach column `cover` at least: the product that forward and
 // backward share.
 static int logits_product(const CeSpace& s, int rows, int D, const uint16_t* w, long long w_stride, long long width, long long cover, int nt,
@@ -721,10 +769,12 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         uint16_t* dw = (uint16_t*)dweight + v0 * dweight_stride;
         WeightEpilogue::Params ew = {{}, dw, dweight_stride, s.top_weight, (int)width, D};
         if (!gemm::encode_map(&ew.out, gemm::kElemBf16, dw, D < 8 ? 8 : D & ~7, width, dweight_stride * 2, 32)) return TSLT_ERR_CUDA;
-        const int rc = s.pair ? gemm::launch_two<false, 2, 4, HiddenEpilogue, WeightEpilogue>(maps, p, eh, maps2, p2, ew, true, st)
-                              : gemm::launch_two<false, 1, 4, HiddenEpilogue, WeightEpilogue>(maps, p, eh, maps2, p2, ew, true, st);
+        const int wide = ((uintptr_t)dhidden & 31) == 0 && dhidden_stride % 16 == 0;
+        const HiddenRowsEpilogue::Params er = {(uint16_t*)dhidden, s.row_of, s.top_weight, dhidden_stride, D, wide};
+        const int rc = s.direct ? both<HiddenRowsEpilogue>(s.pair, maps, p, er, maps2, p2, ew, st) : both<HiddenEpilogue>(s.pair, maps, p, eh, maps2, p2, ew, st);
         if (rc) return rc;
     }
+    if (s.direct) return TSLT_OK;
     const dim3 grid((rows + 31) / 32, (D + 63) / 64);
     return s.splits >= 8 ? launch_after(ce_scatter_kernel<4>, grid, 1024, st, s, (uint16_t*)dhidden, dhidden_stride, D)
                          : launch_after(ce_scatter_kernel<1>, grid, 256, st, s, (uint16_t*)dhidden, dhidden_stride, D);
