@@ -1005,6 +1005,7 @@ def sparsify_hidden(x: torch.Tensor, norm_weight: Optional[torch.Tensor], head: 
     return o
 
 
+@functools.lru_cache(maxsize=256)  # sizes only
 def _loss_workspace_bytes(name: str, rows: int, V: int, D: int) -> int:
     n = ctypes.c_size_t(0)
     _check(getattr(lib(), name)(rows, V, D, ctypes.byref(n)), name)
@@ -1040,13 +1041,18 @@ def linear_ce(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, 
     Returns dict(loss [rows], lse [rows] fp32, workspace), both 0 in ignored rows."""
     dev, rows, V, D, hs, wstride = _loss_inputs(hidden, weight, target)
     device = hidden.device
-    o = {} if out is None else out
-    for name in ("loss", "lse"):
-        if _given(o, name, (rows,), torch.float32, dev) is None:
-            o[name] = torch.empty(rows, dtype=torch.float32, device=device)
-    ws = _space(ws, linear_ce_workspace_bytes(rows, V, D), device, dev)
-    _check(lib().tslt_linear_ce(_at(hidden), hs, _at(weight), wstride, _at(target), rows, V, D, _at(o["loss"]),
-                                _at(o["lse"]), _at(ws), ws.numel(), _stream_on(dev)), "tslt_linear_ce")
+    if out is None:
+        loss, lse = torch.empty(rows, dtype=torch.float32, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+        o = {"loss": loss, "lse": lse}
+    else:
+        o = out
+        for name in ("loss", "lse"):
+            if _given(o, name, (rows,), torch.float32, dev) is None:
+                o[name] = torch.empty(rows, dtype=torch.float32, device=device)
+        loss, lse = o["loss"], o["lse"]
+    ws = _space(ws, _loss_workspace_bytes("tslt_linear_ce_workspace_bytes", rows, V, D), device, dev)
+    _check(lib().tslt_linear_ce(hidden.data_ptr(), hs, weight.data_ptr(), wstride, target.data_ptr(), rows, V, D, loss.data_ptr(),
+                                lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(dev)), "tslt_linear_ce")
     o["workspace"] = ws
     return o
 
@@ -1063,14 +1069,20 @@ def linear_ce_backward(hidden: torch.Tensor, weight: torch.Tensor, target: torch
     _vector(lse, "lse", torch.float32, dev, rows)
     if dloss is not None:
         _vector(dloss, "dloss", torch.float32, dev, rows)
-    o = {} if out is None else out
-    for name, t in (("dhidden", hidden), ("dweight", weight)):
-        if _given(o, name, t.shape, torch.bfloat16, dev) is None:
-            o[name] = _like(t, torch.bfloat16, D)
-    dhs, dws = _stride(o["dhidden"], D, "dhidden"), _stride(o["dweight"], D, "dweight")
-    ws = _space(ws, linear_ce_backward_workspace_bytes(rows, V, D), device, dev)
-    _check(lib().tslt_linear_ce_backward(_at(hidden), hs, _at(weight), wstride, _at(target), _at(lse), _at(dloss), rows, V, D,
-                                         _at(o["dhidden"]), dhs, _at(o["dweight"]), dws, _at(ws), ws.numel(), _stream_on(dev)),
+    if out is None and D % 16 == 0 and hidden.is_contiguous() and weight.is_contiguous():
+        dh, dw = torch.empty_like(hidden), torch.empty_like(weight)
+        dhs = dws = D
+        o = {"dhidden": dh, "dweight": dw}
+    else:
+        o = {} if out is None else out
+        for name, t in (("dhidden", hidden), ("dweight", weight)):
+            if _given(o, name, t.shape, torch.bfloat16, dev) is None:
+                o[name] = _like(t, torch.bfloat16, D)
+        dh, dw = o["dhidden"], o["dweight"]
+        dhs, dws = _stride(dh, D, "dhidden"), _stride(dw, D, "dweight")
+    ws = _space(ws, _loss_workspace_bytes("tslt_linear_ce_backward_workspace_bytes", rows, V, D), device, dev)
+    _check(lib().tslt_linear_ce_backward(hidden.data_ptr(), hs, weight.data_ptr(), wstride, target.data_ptr(), lse.data_ptr(), _at(dloss),
+                                         rows, V, D, dh.data_ptr(), dhs, dw.data_ptr(), dws, ws.data_ptr(), ws.numel(), _stream_on(dev)),
            "tslt_linear_ce_backward")
     o["workspace"] = ws
     return o
