@@ -241,7 +241,7 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
         p.m_tiles = (rows + 255) / 256;
         p.nt = gemm::choose_nt(p.m_tiles, V, true, HeadRowsEpilogue<T>::kCols);
         p.n_tiles = (V + p.nt - 1) / p.nt;
-        p.group_m = 16;
+        p.group_m = gemm::rows_in_l2(256, K);
         p.m_total = rows;
         typename HeadRowsEpilogue<T>::Params ep = {{}, out, out_stride, qs, ws, rows, V};
         const int step = 16 / sizeof(T);
