@@ -4,12 +4,16 @@
 // Mathematics.  z = H W^T; lse_n = ln sum_v exp z[n, v]; loss_n = lse_n - z[n, t_n].  With g_n the weight of row n's loss,
 // G[n, v] = g_n (exp(z[n, v] - lse_n) - [v = t_n]), dH = G W, dW = G^T H.
 //
-// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way.  One product whose epilogue turns each 256-column tile of z, still in tensor memory, into a running (max, sum)
-// pair per row; the pairs of all tiles (8 bytes for 256 logits) go to the workspace and a small kernel joins them.
+// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way.  One product whose
+// epilogue turns each tile of z, still in tensor memory, into (max, sum) pairs, two a row; the pairs of all tiles (16 bytes
+// for 256 logits) go to the workspace and a small kernel joins them.
 // Backward, piece by piece of the vocabulary: z of the piece is computed again and its epilogue writes G of the piece in
-// bf16 to the workspace (as 64-column panels, contiguous whichever of its axes a product reads along); two products read it, dW of the piece (complete: its sum runs over the rows) and the piece's part
-// of dH (summed over the pieces in fp32, in a fixed order).  Bound by the tensor cores: 2 + 6 products of rows x V x D
-// multiply-adds (the recomputation is the price of not keeping rows x V logits).
+// bf16 to the workspace (as 64-column panels, contiguous whichever of its axes a product reads along); one kernel with two
+// products reads it: the piece's part of dH (summed over the pieces in fp32, in a fixed order) and dW of the piece (complete:
+// its sum runs over the rows).  2 + 6 rows x V x D operations; the recomputation is the price of not keeping rows x V logits.
+//
+// Bound by the tensor cores under the power cap (6144 rows, V = 128256, D = 4096, sustained: forward 4.9 ms, a piece of 16128
+// entries z and G 655 us, dH and dW 1250 us; cuBLAS for the three products of a piece alone 627, 612 and 591 us).
 //
 // Ignored rows (negative target) are taken out before anything is multiplied: the rows that count are copied together, in
 // their order, and every product runs over those only.  Ignored rows cost nothing and what they hold (padding, NaN) is

@@ -132,7 +132,7 @@ def head_case(rows, V, D, seed):
 
 @pytest.mark.parametrize("logits", [F32, BF16])
 @pytest.mark.parametrize("rows,V,D", [(1, 1, 1), (1, 1000, 64), (2, 4099, 77), (3, 20011, 1601), (4, 515, 4096), (4, 1003, 12000), (5, 1003, 100), (16, 128, 128), (17, 129, 100), (33, 20011, 1601), (64, 4099, 2048),
-                                      (65, 4099, 2048), (100, 300, 17), (256, 33000, 512), (257, 1027, 640), (700, 5001, 333)])
+                                      (65, 4099, 2048), (100, 300, 17), (129, 5003, 257), (160, 1001, 300), (161, 1001, 300), (256, 33000, 512), (257, 1027, 640), (700, 5001, 333)])
 def test_head_logits(rows, V, D, logits):
     q, w, s, t, want = head_case(rows, V, D, rows + V + D)
     step = 8 if logits == BF16 else 4
