@@ -5,8 +5,9 @@
 // q = rint(127 y / max|y|) with scale = max|y| / 127.  The row's 1 / rms cancels out of q: q = rint(127 v / max|v|).
 // So the sum of squares and the maximum are needed from ONE pass over the row and one block reduction gives both;
 // the row stays in registers between them and is read and written once: 2 + 2 + 2 + 1 bytes an element (bf16 with a
-// residual).  Bound by HBM once the arithmetic was on pairs: 16384 x 4096 takes 91 us (5.2 TB/s), with values 102 us
-// (5.9 TB/s); element by element it was 113 us at 42 instructions an element.  fp32: 129 us, 6.8 TB/s.
+// residual).  Bound by HBM once the arithmetic was on pairs: 16384 x 4096 takes 83 us (5.6 TB/s), with values 95 us
+// (6.4 TB/s, 0.97 of the copy bandwidth); element by element it was 113 us at 42 instructions an element, and 102 us with
+// 76 registers a thread instead of 64 (six CTAs of 128 threads on an SM instead of eight).  fp32: 129 us, 6.8 TB/s.
 //
 // Rounding.  t = v * (127 / max|v|) in fp32 is off by at most 1.5 * 2^-23 * 127 = 2.3e-5; where t lies within 1e-4 of
 // the border between two codes (one element in 5000), the code is taken from the quotient in fp64 instead, so that
@@ -132,7 +133,7 @@ template <typename T> __device__ __forceinline__ void store_elems(void* row, int
 
 // One CTA per row; thread t holds vectors t, t + nthreads, ... (NV of them).
 template <typename T, int NV, bool kNorm>
-__global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024) norm_quant_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * Elt<T>::kPerVec == 32 ? 2 : 0) norm_quant_kernel(const __grid_constant__ NormParams p) {
     constexpr int P = Elt<T>::kPerVec;
     __shared__ float s_sum[32], s_top[32];
     const int tid = threadIdx.x, nth = blockDim.x, nwarps = nth >> 5;
@@ -257,7 +258,7 @@ constexpr int kMaxHidden = TSLT_MAX_HIDDEN;
 template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cudaStream_t st) {
     const int nvec = (p.D + Elt<T>::kPerVec - 1) / Elt<T>::kPerVec;
     // Few rows: latency counts, so a row is spread over as many threads as it has vectors.  Rows enough to fill the
-    // machine: four vectors in flight per thread where a row has 512 (16384 x 4096, us, 1 / 2 / 4 vectors: bf16 118 / 107 / 102,
+    // machine: four vectors in flight per thread where a row has 512 (16384 x 4096, us, 1 / 2 / 4 vectors: bf16 118 / 107 / 95,
     // fp32 329 / 185 / 150).
     int nv = p.rows < 2 * 148 ? 1 : (nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1);
     while ((nvec + nv - 1) / nv > 1024) nv *= 2;
