@@ -526,11 +526,32 @@ inline uint32_t instruction_desc(bool int8, int m, int n, bool a_mn, bool b_mn) 
     return d << 4 | ab << 7 | ab << 10 | (a_mn ? 1u << 15 : 0) | (b_mn ? 1u << 16 : 0) | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
-// Fills idesc and stages from nt, launches on min(tiles, SMs) clusters.  dependent: the kernel before it on the stream is
-// this call's own and its results are waited for inside (programmatic launch).
+// A kernel that waits for the one before it on the stream itself (wait_for_primary_kernel() before it touches global memory), so
+// that its launch and set-up overlap that kernel's end, whatever kernel that is: one that never allows dependents early
+// simply ends first.
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
+// Fills idesc and stages from nt, launches on min(tiles, SMs) clusters.
 template <bool kInt8, int kCtas, int kEpiWarps, class Epi, class Epi2>
 int launch_two(const Maps& maps, Product p, const typename Epi::Params& ep, const Maps& maps2, Product p2, const typename Epi2::Params& ep2,
-               bool dependent, cudaStream_t st) {
+               cudaStream_t st) {
     constexpr bool kDual = !std::is_same<Epi2, NoEpilogue>::value;
     const int sms = sm_count();
     if (sms <= 0) return TSLT_ERR_CUDA;
@@ -552,25 +573,13 @@ int launch_two(const Maps& maps, Product p, const typename Epi::Params& ep, cons
     if (tiles + tiles2 <= 0) return TSLT_OK;
     if (tiles > 0x3fffffffLL || tiles2 > 0x3fffffffLL) return TSLT_ERR_UNSUPPORTED;
     const long long clusters = tiles + tiles2 < sms / kCtas ? tiles + tiles2 : sms / kCtas;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(clusters * kCtas), 1, 1);
-    cfg.blockDim = dim3(64 + 32 * kEpiWarps, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = dependent;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kCtas;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = kCtas > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, maps, p, ep, maps2, p2, ep2) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    return launch_early(kern, dim3((unsigned)(clusters * kCtas)), 64 + 32 * kEpiWarps, smem, kCtas, st, maps, p, ep, maps2, p2, ep2) == cudaSuccess
+               ? TSLT_OK
+               : TSLT_ERR_CUDA;
 }
 template <bool kInt8, int kCtas, int kEpiWarps, class Epi>
-int launch(const Maps& maps, const Product& p, const typename Epi::Params& ep, bool dependent, cudaStream_t st) {
-    return launch_two<kInt8, kCtas, kEpiWarps, Epi, NoEpilogue>(maps, p, ep, maps, p, NoEpilogue::Params{}, dependent, st);
+int launch(const Maps& maps, const Product& p, const typename Epi::Params& ep, cudaStream_t st) {
+    return launch_two<kInt8, kCtas, kEpiWarps, Epi, NoEpilogue>(maps, p, ep, maps, p, NoEpilogue::Params{}, st);
 }
 
 // The column width of a tile, a multiple of `unit`, at most 256: the one whose rounds of tiles over the machine's clusters cost

@@ -142,6 +142,8 @@ template <int kRows, typename T>
 __global__ void __launch_bounds__(kVecThreads, 4) head_vec_kernel(const __grid_constant__ VecParams p) {
     extern __shared__ __align__(16) uint8_t s_codes[];
     const int tid = threadIdx.x, lane = tid & 31;
+    wait_for_primary_kernel();
+    allow_dependent_launch();
     const int chunks = (p.K + 15) / 16;  // a row's last 16 bytes may hold anything behind K: they meet zeros
     if (blockIdx.x == 0 && tid == 0) *p.status = 0;  // nothing here waits
     for (int i = tid; i < kRows * chunks; i += kVecThreads) {
@@ -218,8 +220,10 @@ template <int kRows, typename T> static int launch_vec(VecParams p, int* status,
     const int sms = gemm::sm_count();
     if (sms <= 0) return TSLT_ERR_CUDA;
     const long long most = (long long)sms * 4;
-    head_vec_kernel<kRows, T><<<(unsigned)(blocks < most ? blocks : most), kVecThreads, (size_t)kRows * ((p.K + 15) / 16 * 16), st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    return gemm::launch_early(head_vec_kernel<kRows, T>, dim3((unsigned)(blocks < most ? blocks : most)), kVecThreads,
+                              (size_t)kRows * ((p.K + 15) / 16 * 16), 1, st, p) == cudaSuccess
+               ? TSLT_OK
+               : TSLT_ERR_CUDA;
 }
 
 // Rows from which the tokens become the tensor cores' rows: few-rows / many-rows form, us, at V = 128256, K = 4096: 128 rows
@@ -253,7 +257,7 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
             !gemm::encode_map(&ep.out, sizeof(T) == 4 ? gemm::kElemFp32 : gemm::kElemBf16, out, V < step ? step : V / step * step, rows,
                               out_stride * (long long)sizeof(T), 32))
             return TSLT_ERR_CUDA;
-        return gemm::launch<true, 2, 4, HeadRowsEpilogue<T>>(maps, p, ep, false, st);
+        return gemm::launch<true, 2, 4, HeadRowsEpilogue<T>>(maps, p, ep, st);
     }
     p.nt = rows <= 16 ? 16 : (rows + 31) / 32 * 32;
     p.n_tiles = 1;
@@ -262,7 +266,7 @@ static int launch_head(const signed char* q, const float* qs, long long q_stride
     p.m_total = V;
     if (!gemm::encode_map(&maps.a, gemm::kElemInt8, w, K, V, w_stride, 128) || !gemm::encode_map(&maps.b, gemm::kElemInt8, q, K, rows, q_stride, p.nt)) return TSLT_ERR_CUDA;
     const typename HeadEpilogue<T>::Params ep = {out, out_stride, qs, ws, rows, V};
-    return gemm::launch<true, 1, 8, HeadEpilogue<T>>(maps, p, ep, false, st);
+    return gemm::launch<true, 1, 8, HeadEpilogue<T>>(maps, p, ep, st);
 }
 
 }  // namespace tslt

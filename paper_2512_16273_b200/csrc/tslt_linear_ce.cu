@@ -143,6 +143,7 @@ __device__ __forceinline__ uint4 row_vec(const uint16_t* row, int i, int D) {
 __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_constant__ GatherParams p) {
     __shared__ int s_before, s_all;
     __shared__ uint32_t s_top;
+    wait_for_primary_kernel();
     allow_dependent_launch();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int first = min(p.rows, (int)blockIdx.x * p.per), last = min(p.rows, first + p.per);
@@ -601,37 +602,27 @@ __global__ void __launch_bounds__(256 * kGroups) ce_scatter_kernel(CeSpace s, ui
 }
 
 // ---- host --------------------------------------------------------------------------------------------------
+template <typename... Params, typename... Args>
+static int launch_after(void (*kernel)(Params...), dim3 grid, int threads, cudaStream_t st, const Args&... args) {
+    return gemm::launch_early(kernel, grid, threads, 0, 1, st, args...) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+}
+
 static int gather(GatherParams p, cudaStream_t st) {
     p.per = p.rows > 8 * 148 * 8 ? (p.rows + 148 * 8 - 1) / (148 * 8) : 8;
     const int grid = (p.rows + p.per - 1) / p.per;
-    ce_gather_kernel<<<grid, kGatherThreads, 0, st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
-}
-
-template <typename... Args>
-static int launch_after(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads, 1, 1);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    return launch_after(ce_gather_kernel, dim3(grid), kGatherThreads, st, p);
 }
 
 template <class Epi, int kWarps>
 static int product(bool pair, const gemm::Maps& maps, const gemm::Product& p, const typename Epi::Params& ep, cudaStream_t st) {
-    return pair ? gemm::launch<false, 2, kWarps, Epi>(maps, p, ep, true, st) : gemm::launch<false, 1, kWarps, Epi>(maps, p, ep, true, st);
+    return pair ? gemm::launch<false, 2, kWarps, Epi>(maps, p, ep, st) : gemm::launch<false, 1, kWarps, Epi>(maps, p, ep, st);
 }
 
 template <class Epi>
 static int both(bool pair, const gemm::Maps& maps, const gemm::Product& p, const typename Epi::Params& ep, const gemm::Maps& maps2,
                 const gemm::Product& p2, const WeightEpilogue::Params& ep2, cudaStream_t st) {
-    return pair ? gemm::launch_two<false, 2, 4, Epi, WeightEpilogue>(maps, p, ep, maps2, p2, ep2, true, st)
-                : gemm::launch_two<false, 1, 4, Epi, WeightEpilogue>(maps, p, ep, maps2, p2, ep2, true, st);
+    return pair ? gemm::launch_two<false, 2, 4, Epi, WeightEpilogue>(maps, p, ep, maps2, p2, ep2, st)
+                : gemm::launch_two<false, 1, 4, Epi, WeightEpilogue>(maps, p, ep, maps2, p2, ep2, st);
 }
 
 // z of `width` vocabulary entries of the weight, in tiles that reach column `cover` at least: the product that forward and

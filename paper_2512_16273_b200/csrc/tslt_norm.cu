@@ -13,7 +13,7 @@
 // the border between two codes (one element in 5000), the code is taken from the quotient in fp64 instead, so that
 // every code is the nearest one to the exact quotient of the fp32 values v and max|v|.  (For bf16 h and w the product
 // v is exact.)
-#include "tslt_common.cuh"
+#include "tslt_gemm.cuh"
 
 namespace tslt {
 
@@ -136,6 +136,8 @@ template <typename T, int NV, bool kNorm>
 __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * Elt<T>::kPerVec == 32 ? 2 : 0) norm_quant_kernel(const __grid_constant__ NormParams p) {
     constexpr int P = Elt<T>::kPerVec;
     __shared__ float s_sum[32], s_top[32];
+    wait_for_primary_kernel();
+    allow_dependent_launch();
     const int tid = threadIdx.x, nth = blockDim.x, nwarps = nth >> 5;
     const long long row = blockIdx.x;
     const char* x = (const char*)p.x + row * p.xs * Elt<T>::kBytes;
@@ -263,10 +265,8 @@ template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cu
     int nv = p.rows < 2 * 148 ? 1 : (nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1);
     while ((nvec + nv - 1) / nv > 1024) nv *= 2;
     const int threads = ((nvec + nv - 1) / nv + 31) / 32 * 32;
-    if (nv == 1) norm_quant_kernel<T, 1, kNorm><<<p.rows, threads, 0, st>>>(p);
-    else if (nv == 2) norm_quant_kernel<T, 2, kNorm><<<p.rows, threads, 0, st>>>(p);
-    else norm_quant_kernel<T, 4, kNorm><<<p.rows, threads, 0, st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    auto kern = nv == 1 ? norm_quant_kernel<T, 1, kNorm> : nv == 2 ? norm_quant_kernel<T, 2, kNorm> : norm_quant_kernel<T, 4, kNorm>;
+    return gemm::launch_early(kern, dim3(p.rows), threads, 0, 1, st, p) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
 }
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }

@@ -474,3 +474,69 @@ def test_from_hidden_states_to_drafts_and_verification(B, gamma, logits):
     rv = oracle.verify(zc, ref["idx"].reshape(B, gamma, k), ref["logit"].reshape(B, gamma, k), ref["count"].reshape(B, gamma), tok, T, T,
                        ua.numpy(), us.numpy())
     compare_verify(v, rv, "hidden", inputs=verify_inputs(zc, ref, B, gamma, k, tok, T, T, ua, us))
+
+
+def slow_copy(dst, src, work):
+    """dst = src, behind a few milliseconds of products on the same stream."""
+    for _ in range(4):
+        work @ work
+    dst.copy_(src)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_inputs_written_on_another_stream(captured):
+    """Calls whose inputs another stream writes, waited for by an event right before the call (the calls' kernels are launched
+    ahead of the end of the kernel before them: an event in between has to hold them back)."""
+    q, w, s, t, _ = head_case(70, 9000, 512, 41)
+    h, lw, lt, dl = loss_case(70, 3000, 512, 0.1, 42)
+    x = torch.randn(300, 512, device="cuda").to(BF16)
+
+    def calls(a):
+        z = tslt.head_logits(a["q"], s, w, t)["logits"]
+        v = tslt.head_logits(a["q"][:3], s[:3], w, t)["logits"]
+        f = tslt.linear_ce(a["h"], lw, lt)
+        g = tslt.linear_ce_backward(a["h"], lw, lt, f["lse"], dl)
+        n = tslt.rmsnorm_quant(a["x"])
+        return [z, v, f["loss"], g["dhidden"], g["dweight"], n["q"], n["scale"]]
+    want = [o.clone() for o in calls({"q": q, "h": h, "x": x})]
+    buf = {"q": torch.zeros_like(q), "h": torch.zeros_like(h), "x": torch.zeros_like(x)}
+    work = torch.randn(4096, 4096, device="cuda").to(BF16)
+    side = torch.cuda.Stream()
+
+    def once():
+        out = []
+        here = torch.cuda.current_stream()
+        for k, src in (("q", q), ("h", h), ("x", x)):
+            side.wait_stream(here)
+            with torch.cuda.stream(side):
+                slow_copy(buf[k], src, work)
+            tslt.quantize_rows(x)  # a kernel of the library right before the wait
+            here.wait_stream(side)
+            if k == "q":
+                out += [tslt.head_logits(buf[k], s, w, t)["logits"]]
+            elif k == "h":
+                f = tslt.linear_ce(buf[k], lw, lt)
+                g = tslt.linear_ce_backward(buf[k], lw, lt, f["lse"], dl)
+                out += [tslt.head_logits(buf["q"][:3], s[:3], w, t)["logits"], f["loss"], g["dhidden"], g["dweight"]]
+            else:
+                n = tslt.rmsnorm_quant(buf[k])
+                out += [n["q"], n["scale"]]
+        return out
+    if captured:
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            work @ work  # the product's own workspace exists before the capture
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = once()
+    for _ in range(3):
+        for b in buf.values():
+            b.zero_()
+        if captured:
+            graph.replay()
+        else:
+            out = once()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(out, want)):
+            assert torch.equal(a, b), i
