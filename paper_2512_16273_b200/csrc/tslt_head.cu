@@ -3,8 +3,8 @@
 //
 // One to four rows (a draft's step): bound by reading the weight once and by how soon that starts.  No tensor cores: warps take
 // blocks of four weight rows, each lane 16 bytes of k at a time from all four, and dot products of four bytes (dp4a) with
-// the tokens' codes in shared memory.  V = 32000, K = 2048, us with / without this form: 1 row 14.4 / 18.8, 4 rows
-// 15.8 / 18.8, 8 rows 23.0 / 19.4 (the dot products are then the bound); V = 128256, K = 4096: 1 row 80 / 87, 4 rows 83 / 91.
+// the tokens' codes in shared memory.  V = 32000, K = 2048, us with / without this form: 1 row 12.8 / 17.6, 4 rows
+// 14.1 / 17.6, 8 rows 23.0 / 17.6 (the dot products are then the bound); V = 128256, K = 4096: 1 row 78 / 87, 4 rows 82 / 88.
 //
 // Few rows (a decoding step): bound by reading the weight once.  The weight is the operand of the tensor cores' 128 rows and
 // the tokens are its columns (16 ... 160), so that the whole weight goes once through shared memory whatever their number
