@@ -394,9 +394,8 @@ int tslt_quantize_rows(const void* x, int dtype, int rows, int D, long long x_st
  * weight_scale) and the result is rounded once to logits_dtype (TSLT_F32 or TSLT_BF16).  The logits are laid out as
  * tslt_sparsify, tslt_verify and tslt_tree_verify read them.
  * q [rows, D] and weight [V, D] int8 (-128 is allowed), logits [rows, V], each with a row stride (elements); base pointers
- * 16-byte aligned, strides multiples of 16 bytes; rows, V and D need not be multiples of anything; D <= TSLT_MAX_INT8_K, rows and
- * V <= TSLT_MAX_VOCAB.  Elements between
- * V and logits_stride are left as they are.  Workspace >= 256 bytes (the status word), 256-byte aligned.
+ * 16-byte aligned, strides multiples of 16 bytes; rows, V and D need not be multiples of anything; D <= TSLT_MAX_INT8_K,
+ * rows and V <= TSLT_MAX_VOCAB.  Elements between V and logits_stride are left as they are.  Workspace >= 256 bytes (the status word), 256-byte aligned.
  */
 int tslt_head_logits(const signed char* q, const float* q_scale, long long q_stride, const signed char* weight,
                      const float* weight_scale, long long weight_stride, int rows, int V, int D, int logits_dtype,
@@ -412,7 +411,8 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  * G[n, v] = dloss[n] (exp(z[n, v] - lse[n]) - [v = target[n]]) (0 in ignored rows),
  *   dhidden = G weight,  dweight = G^T hidden,
  * both overwritten whole (zeros for ignored rows; zeros in dweight when no row counts).  lse is what tslt_linear_ce
- * wrote.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
+ * wrote.  A NaN or an infinity in a row that counts, or logits that overflow fp32, make that row's loss, lse and
+ * dhidden not finite, and dweight with them; other rows keep theirs.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
  * own rounding) and counts as 0 below 2^-126; sums are fp32 and their order is fixed: the same inputs give the same bits.
  * hidden, dhidden [rows, D], weight, dweight [V, D]: bf16 with row strides (elements, multiples of 8), 16-byte aligned;
  * target [rows] int32; loss, lse, dloss [rows] fp32.  rows = 0 is allowed (dweight = 0).  D <= TSLT_MAX_HIDDEN, rows <=
