@@ -131,15 +131,16 @@ template <typename T> __device__ __forceinline__ void store_elems(void* row, int
     }
 }
 
-// One CTA per row; thread t holds vectors t, t + nthreads, ... (NV of them).
-template <typename T, int NV, bool kNorm>
+// A row is a CTA's, or (kWarpRow, narrow rows) a warp's with nothing to meet for; thread t of it holds vectors t, t + nthreads, ... (NV of them).
+template <typename T, int NV, bool kNorm, bool kWarpRow>
 __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * Elt<T>::kPerVec == 32 ? 2 : 0) norm_quant_kernel(const __grid_constant__ NormParams p) {
     constexpr int P = Elt<T>::kPerVec;
     __shared__ float s_sum[32], s_top[32];
     wait_for_primary_kernel();
     allow_dependent_launch();
-    const int tid = threadIdx.x, nth = blockDim.x, nwarps = nth >> 5;
-    const long long row = blockIdx.x;
+    const int tid = kWarpRow ? threadIdx.x & 31 : threadIdx.x, nth = kWarpRow ? 32 : blockDim.x, nwarps = nth >> 5;
+    const long long row = kWarpRow ? (long long)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32 : blockIdx.x;
+    if (kWarpRow && row >= p.rows) return;
     const char* x = (const char*)p.x + row * p.xs * Elt<T>::kBytes;
     const char* r = p.r ? (const char*)p.r + row * p.rs * Elt<T>::kBytes : nullptr;
     uint4 xv[NV], rv[NV], wv[NV];  // every load of the row is in flight before the first is used
@@ -184,16 +185,18 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * 
     float sum = lo_of(squares) + hi_of(squares);
     sum = warp_sum(sum);
     top = warp_max(top);
-    if ((tid & 31) == 0) {
-        s_sum[tid >> 5] = sum;
-        s_top[tid >> 5] = top;
-    }
-    __syncthreads();
-    sum = 0.f;
-    top = 0.f;
-    for (int w = 0; w < nwarps; ++w) {  // the same order in every thread
-        sum += s_sum[w];
-        top = fmaxf(top, s_top[w]);
+    if (!kWarpRow) {
+        if ((tid & 31) == 0) {
+            s_sum[tid >> 5] = sum;
+            s_top[tid >> 5] = top;
+        }
+        __syncthreads();
+        sum = 0.f;
+        top = 0.f;
+        for (int w = 0; w < nwarps; ++w) {  // the same order in every thread
+            sum += s_sum[w];
+            top = fmaxf(top, s_top[w]);
+        }
     }
     float s = top / 127.f;
     if (kNorm) s = top == 0.f && sum == sum ? 0.f : s / sqrtf(sum / (float)p.D + p.eps);
@@ -262,10 +265,15 @@ template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cu
     // Few rows: latency counts, so a row is spread over as many threads as it has vectors.  Rows enough to fill the
     // machine: four vectors in flight per thread where a row has 512 (16384 x 4096, us, 1 / 2 / 4 vectors: bf16 118 / 107 / 95,
     // fp32 329 / 185 / 150).
-    int nv = p.rows < 2 * 148 ? 1 : (nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1);
+    const bool many = p.rows >= 2 * 148;
+    if (many && nvec <= 128) {  // a warp holds the row: no barrier, and a quarter of the CTAs to start (16384 x 512 bf16: 18.1 -> 14.8 us)
+        auto kern = nvec > 64 ? norm_quant_kernel<T, 4, kNorm, true> : nvec > 32 ? norm_quant_kernel<T, 2, kNorm, true> : norm_quant_kernel<T, 1, kNorm, true>;
+        return gemm::launch_early(kern, dim3((p.rows + 3) / 4), 128, 0, 1, st, p) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
+    }
+    int nv = !many ? 1 : nvec >= 512 ? 4 : nvec >= 256 ? 2 : 1;
     while ((nvec + nv - 1) / nv > 1024) nv *= 2;
     const int threads = ((nvec + nv - 1) / nv + 31) / 32 * 32;
-    auto kern = nv == 1 ? norm_quant_kernel<T, 1, kNorm> : nv == 2 ? norm_quant_kernel<T, 2, kNorm> : norm_quant_kernel<T, 4, kNorm>;
+    auto kern = nv == 1 ? norm_quant_kernel<T, 1, kNorm, false> : nv == 2 ? norm_quant_kernel<T, 2, kNorm, false> : norm_quant_kernel<T, 4, kNorm, false>;
     return gemm::launch_early(kern, dim3(p.rows), threads, 0, 1, st, p) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
 }
 

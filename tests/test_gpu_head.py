@@ -51,7 +51,8 @@ def norm_reference(x, r, w, eps):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,D", [(1, 1), (1, 4096), (3, 7), (5, 129), (2, 16384), (700, 1000), (301, 4097), (1, 5120), (400, 64)])
+@pytest.mark.parametrize("rows,D", [(1, 1), (1, 4096), (3, 7), (5, 129), (2, 16384), (700, 1000), (301, 4097), (1, 5120), (400, 64),
+                                    (299, 257), (1001, 511), (297, 1024), (303, 8)])
 @pytest.mark.parametrize("residual", [True, False])
 def test_rmsnorm_quant(dtype, rows, D, residual):
     g = gen(rows * 31 + D)
