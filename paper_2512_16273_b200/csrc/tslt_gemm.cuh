@@ -60,14 +60,9 @@ struct Product {
     int* status;
 };
 
-struct WarpSmem {  // an epilogue warp's own shared memory: kBoxes output boxes used in turn, and a scratch
+struct WarpSmem {  // an epilogue warp's own shared memory: two output boxes used in turn, and a scratch
     uint32_t box, scratch;
     int turn;
-    __device__ __forceinline__ uint32_t next() {
-        const uint32_t b = box + turn * 4096;
-        turn ^= 1;
-        return b;
-    }
 };
 
 struct Tile {
@@ -229,16 +224,31 @@ __device__ __forceinline__ uint32_t tmem_ld1(uint32_t addr) {  // one column, wa
     return v;
 }
 
-// An epilogue warp's output box: 32 rows of 64 bf16 columns, written with the 128-byte swizzle (16-byte chunk i of row r at
-// chunk i ^ (r mod 8)) and sent off by one lane as one copy, which clips it at the matrix's edges.
-__device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t box, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(box) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
 template <int kPending> __device__ __forceinline__ void store_wait_read() {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kPending) : "memory");
 }
 __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// An epilogue warp's output box: 32 rows of 128 bytes (lane l's row in b), written with the 128-byte swizzle (16-byte chunk i of row r
+// at chunk i ^ (r mod 8)) and sent off by one lane as one copy, which clips it at the matrix's edges.  The boxes change at a copy and at
+// nothing else, so that "all copies but the newest have read their box" always speaks of this box: what is not copied out takes no box.
+__device__ __forceinline__ void send_box(WarpSmem& own, const uint32_t* b, int lane, const CUtensorMap* map, int x, int y) {
+    if (lane == 0) store_wait_read<1>();
+    __syncwarp();
+    const uint32_t box = own.box + own.turn * kStageOut, line = box + lane * 128;
+    own.turn ^= 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
+                     "r"(b[4 * i + 2]), "r"(b[4 * i + 3])
+                     : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(box) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
 
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, 8-row groups 1024 bytes apart (sbo).
 // MN-major: 64 contiguous elements of m per 128-byte row, one row per k; 8-k groups 1024 bytes apart (sbo), the next

@@ -102,17 +102,7 @@ template <typename T> struct HeadRowsEpilogue {
                     }
                 }
             }
-            if (lane == 0) gemm::store_wait_read<1>();  // the last copy but one, which was of this box, has read it
-            __syncwarp();
-            const uint32_t box = own.next(), line = box + lane * 128;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
-                             "r"(b[4 * i + 2]), "r"(b[4 * i + 3])
-                             : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0 && row < p.n_rows && v0 < whole) gemm::store_box(&p.out, box, v0, row);
+            if (row - lane < p.n_rows && v0 < whole) gemm::send_box(own, b, lane, &p.out, v0, row - lane);
             if (whole < p.V && v0 + kCols > whole && row < p.n_rows) {
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) {

@@ -386,18 +386,8 @@ struct WeightEpilogue {
                     if (zero) b[16 * half + j] = 0;
                 }
             }
-            if (lane == 0) gemm::store_wait_read<1>();  // the last copy but one, which was of this box, has read it
-            __syncwarp();
-            const uint32_t box = own.next(), line = box + lane * 128;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + ((i ^ (lane & 7)) << 4)), "r"(b[4 * i]), "r"(b[4 * i + 1]),
-                             "r"(b[4 * i + 2]), "r"(b[4 * i + 3])
-                             : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
             const int d = t.col0 + c, whole = p.D & ~7;
-            if (lane == 0 && row < p.n_real && d < whole) gemm::store_box(&p.out, box, d, row);
+            if (row - lane < p.n_real && d < whole) gemm::send_box(own, b, lane, &p.out, d, row - lane);
             if (whole < p.D && d + 64 > whole && row < p.n_real) {
 #pragma unroll
                 for (int j = 0; j < 64; ++j)
