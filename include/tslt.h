@@ -412,8 +412,9 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  *   dhidden = G weight,  dweight = G^T hidden,
  * both overwritten whole (zeros for ignored rows; zeros in dweight when no row counts).  lse is what tslt_linear_ce
  * wrote.  A NaN or an infinity in a row that counts, or logits that overflow fp32, make that row's loss, lse and
- * dhidden not finite, and dweight with them; other rows keep theirs.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
- * own rounding) and counts as 0 below 2^-126; sums are fp32 and their order is fixed: the same inputs give the same bits.
+ * dhidden not finite, and dweight with them; other rows keep theirs.  So does a dloss that is not finite with its row's
+ * dhidden and with dweight.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
+ * own rounding) and counts as 0 below 2^-126 times the largest finite |dloss|; sums are fp32 and their order is fixed: the same inputs give the same bits.
  * hidden, dhidden [rows, D], weight, dweight [V, D]: bf16 with row strides (elements, multiples of 8), 16-byte aligned;
  * target [rows] int32; loss, lse, dloss [rows] fp32.  rows = 0 is allowed (dweight = 0).  D <= TSLT_MAX_HIDDEN, rows <=
  * TSLT_MAX_LOSS_ROWS, V <= TSLT_MAX_VOCAB.  Outputs must not overlap inputs or each other (the same

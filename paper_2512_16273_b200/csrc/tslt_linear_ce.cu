@@ -37,7 +37,7 @@ struct CeSpace {
     int* count;
     int* row_of;       // [rows_pad] source row of the i-th row that counts
     int* target;       // [rows_pad]
-    float* top_weight; // the largest |g| of the rows that count          (backward)
+    float* top_weight; // the largest finite |g| of the rows that count, 1 if that is 0   (backward)
     float* lse2;       // [rows_pad] lse * log2(e)                        (backward)
     float* weight;     // [rows_pad] g / top_weight                       (backward)
     uint16_t* hidden;  // panels [ds / 64][rows_pad][64]: the rows that count, bf16; zeros up to the next multiple of 256 rows
@@ -174,7 +174,10 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
         bad |= t >= p.V;
         all += c;
         before += i < first ? c : 0;
-        if (p.weight_in && c) top = fmaxf(top, fabsf(__ldg(p.weight_in + i)));
+        if (p.weight_in && c) {
+            const float g = fabsf(__ldg(p.weight_in + i));
+            if (g < INFINITY) top = fmaxf(top, g);  // a NaN or an infinity stays in its own row
+        }
     }
     before = __reduce_add_sync(0xffffffffu, before);
     all = __reduce_add_sync(0xffffffffu, all);
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
         atomicMax(&s_top, __float_as_uint(top));  // non-negative floats order as integers
     }
     __syncthreads();
-    const float wtop = p.weight_in ? __uint_as_float(s_top) : 1.f;
+    const float wtop = p.weight_in && s_top ? __uint_as_float(s_top) : 1.f;
     if (blockIdx.x == 0 && tid == 0) {
         *p.s.status = bad ? TSLT_STATUS_BAD_TARGET : 0;
         *p.s.count = s_all;
@@ -220,7 +223,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
                         p.s.ztarget[at] = z;
                     } else {
                         p.s.lse2[at] = (float)((double)p.lse_in[row] * 1.4426950408889634);
-                        p.s.weight[at] = !p.weight_in ? 1.f : wtop > 0.f ? __fdiv_rn(p.weight_in[row], wtop) : 0.f;
+                        p.s.weight[at] = p.weight_in ? __fdiv_rn(p.weight_in[row], wtop) : 1.f;
                     }
                 }
             } else if (p.loss) {

@@ -10,6 +10,41 @@ from test_gpu_head import BF16, F32, gen, loss_case, loss_reference, padded, wit
 pytestmark = pytest.mark.gpu
 
 
+# ---- dloss --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,V", [(40, 333), (300, 900)])
+@pytest.mark.parametrize("odd", [float("nan"), float("inf"), -float("inf")])
+def test_linear_ce_backward_derivatives_that_are_not_finite(rows, V, odd):
+    """A dloss that is not finite shows in its row's dhidden and in dweight, and in no other row's dhidden."""
+    h, w, t, dl = loss_case(rows, V, 128, 0.2, 4)
+    on = t >= 0
+    f = tslt.linear_ce(h, w, t)
+    i = int(on.nonzero()[1, 0])
+    other = on.clone()
+    other[i] = False
+    # all of them: the usual form, one derivative for every row
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], torch.full_like(dl, odd))
+    assert not g["dhidden"][on].isfinite().any() and not g["dweight"].isfinite().any() and not g["dhidden"][~on].any()
+    # beside zeros
+    one = torch.zeros_like(dl)
+    one[i] = odd
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], one)
+    assert not g["dhidden"][i].isfinite().any() and not g["dweight"].isfinite().any()
+    assert not g["dhidden"][other].any() and g["dhidden"][other].isfinite().all()
+    # beside finite ones: they keep their gradients bit by bit
+    dl[i] = 0.0
+    want = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+    dl[i] = odd
+    g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+    assert not g["dhidden"][i].isfinite().any() and not g["dweight"].isfinite().any()
+    assert torch.equal(g["dhidden"][other], want["dhidden"][other])
+    # in a row that is ignored: nothing
+    if bool((~on).any()):
+        dl[i] = 0.0
+        dl[~on] = odd
+        g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+        assert torch.equal(g["dhidden"], want["dhidden"]) and torch.equal(g["dweight"], want["dweight"])
+
+
 # ---- copies out of every tile -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("logits", [F32, BF16])
 @pytest.mark.parametrize("rows,V", [(640, 128001), (385, 100007), (200, 64 * 1501 + 1), (161, 32 * 3001 + 3), (300, 50000)])
