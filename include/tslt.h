@@ -414,7 +414,9 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  * wrote.  A NaN or an infinity in a row that counts, or logits that overflow fp32, make that row's loss, lse and
  * dhidden not finite, and dweight with them; other rows keep theirs.  So does a dloss that is not finite with its row's
  * dhidden and with dweight.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
- * own rounding) and counts as 0 below 2^-126 times the largest finite |dloss|; sums are fp32 and their order is fixed: the same inputs give the same bits.
+ * own rounding) and counts as 0 below 2^-126 times the largest finite |dloss|; at a
+ * target of probability near 1 it is formed from an fp32 dot product of its own and lse as given, whose fp32 rounding (2^-24 |lse|) then
+ * is an error of that size beside 1 - p.  Sums are fp32 and their order is fixed: the same inputs give the same bits.
  * hidden, dhidden [rows, D], weight, dweight [V, D]: bf16 with row strides (elements, multiples of 8), 16-byte aligned;
  * target [rows] int32; loss, lse, dloss [rows] fp32.  rows = 0 is allowed (dweight = 0).  D <= TSLT_MAX_HIDDEN, rows <=
  * TSLT_MAX_LOSS_ROWS, V <= TSLT_MAX_VOCAB.  Outputs must not overlap inputs or each other (the same

@@ -4,7 +4,9 @@
 // Mathematics.  z = H W^T; lse_n = ln sum_v exp z[n, v]; loss_n = lse_n - z[n, t_n].  With g_n the weight of row n's loss,
 // G[n, v] = g_n (exp(z[n, v] - lse_n) - [v = t_n]), dH = G W, dW = G^T H.
 //
-// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way.  One product whose
+// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way (backward does the same: where
+// the target's probability is near 1, its entry of G is a small difference, which the tensor cores' truncated sum of z would
+// spoil: off by up to 470 times what lse's own rounding leaves, D = 8192).  One product whose
 // epilogue turns each tile of z, still in tensor memory, into (max, sum) pairs, two a row; the pairs of all tiles (16 bytes
 // for 256 logits) go to the workspace and a small kernel joins them.
 // Backward, piece by piece of the vocabulary: z of the piece is computed again and its epilogue writes G of the piece in
@@ -40,6 +42,7 @@ struct CeSpace {
     float* top_weight; // the largest finite |g| of the rows that count, 1 if that is 0   (backward)
     float* lse2;       // [rows_pad] lse * log2(e)                        (backward)
     float* weight;     // [rows_pad] g / top_weight                       (backward)
+    float* gtarget;    // [rows_pad] G at the target / top_weight         (backward)
     uint16_t* hidden;  // panels [ds / 64][rows_pad][64]: the rows that count, bf16; zeros up to the next multiple of 256 rows
     float2* part;      // [parts, rows_pad] (max, sum) in base 2          (forward)
     float* ztarget;    // [rows_pad]                                      (forward)
@@ -92,6 +95,7 @@ static CeSpace ce_space(void* ws, int rows, int V, int D, bool backward) {
     if (backward) {
         s.lse2 = (float*)take(s.rows_pad * 4);
         s.weight = (float*)take(s.rows_pad * 4);
+        s.gtarget = (float*)take(s.rows_pad * 4);
         s.g = (uint16_t*)take(s.rows_pad * s.piece * 2);
         if (!s.direct) s.acc = (float*)take((size_t)s.splits * s.rows_pad * s.da * 4);
     } else {
@@ -158,10 +162,8 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
     auto load = [&](const uint16_t* h, const uint16_t* w, int i0) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = row_vec(h, i0 + 32 * k, p.D);
-        if (p.loss) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = row_vec(w, i0 + 32 * k, p.D);
-        }
+        for (int k = 0; k < 4; ++k) u[k] = row_vec(w, i0 + 32 * k, p.D);
     };
     if (counts(t1, p.V)) load(p.hidden + row1 * p.h_stride, p.weight + t1 * p.w_stride, lane);
     __syncthreads();
@@ -206,16 +208,16 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
                 const uint16_t *h = p.hidden + row * p.h_stride, *w = p.weight + t * p.w_stride;
                 uint4* dst = reinterpret_cast<uint4*>(p.s.hidden) + (size_t)at * 8;
                 float z = 0.f;
-                for (int i0 = lane; i0 < vecs; i0 += 128) {  // four (eight with the weight's row) loads in flight
+                for (int i0 = lane; i0 < vecs; i0 += 128) {  // eight loads in flight
                     if (row != row1 || i0 != lane) load(h, w, i0);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int i = i0 + 32 * k;
-                        if (p.loss) z = dot8(v[k], u[k], z);
+                        z = dot8(v[k], u[k], z);
                         if (i < vecs) dst[(size_t)(i >> 3) * p.s.rows_pad * 8 + (i & 7)] = v[k];
                     }
                 }
-                if (p.loss) z = warp_sum(z);
+                z = warp_sum(z);
                 if (lane == 0) {
                     p.s.row_of[at] = row;
                     p.s.target[at] = t;
@@ -223,7 +225,9 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
                         p.s.ztarget[at] = z;
                     } else {
                         p.s.lse2[at] = (float)((double)p.lse_in[row] * 1.4426950408889634);
-                        p.s.weight[at] = p.weight_in ? __fdiv_rn(p.weight_in[row], wtop) : 1.f;
+                        const float g = p.weight_in ? __fdiv_rn(p.weight_in[row], wtop) : 1.f;
+                        p.s.weight[at] = g;
+                        p.s.gtarget[at] = g * expm1f(z - p.lse_in[row]);
                     }
                 }
             } else if (p.loss) {
@@ -317,7 +321,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and t
     struct Params {
         float log2e;
         uint16_t* g;
-        const float *lse2, *weight;
+        const float *lse2, *weight, *gtarget;
         const int* target;
         long long rows_pad;
         int v0, n_real;  // first vocabulary entry of the piece; its entries
@@ -351,10 +355,9 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and t
         }
         // the target's entry, by the part that wrote its column
         const bool here = col >= 0 && col < n && (col / 32) % kParts == part;
-        const float z = pick_column(tmem, here ? col : -1, lane);
         if (here) {
             uint16_t b;
-            asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"((ex2_approx(fmaf(z, p.log2e, -lse2)) - 1.f) * w));
+            asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"(__ldg(p.gtarget + row)));
             *at(col) = b;
         }
     }
@@ -721,7 +724,7 @@ extern "C" int tslt_linear_ce_backward(const void* hidden, long long hidden_stri
         gemm::Maps maps;
         if (const int rc = logits_product(s, rows, D, w + v0 * weight_stride, weight_stride, width, up(width, 64),  // dH sums in steps of 64
                                          gemm::choose_nt((rows + tile_rows - 1) / tile_rows, width, s.pair != 0, 32), &p, &maps)) return rc;
-        const GradEpilogue::Params eg = {log2e_for(D), s.g, s.lse2, s.weight, s.target, s.rows_pad, (int)v0, (int)width};
+        const GradEpilogue::Params eg = {log2e_for(D), s.g, s.lse2, s.weight, s.gtarget, s.target, s.rows_pad, (int)v0, (int)width};
         if (const int rc = product<GradEpilogue, 8>(s.pair, maps, p, eg, st)) return rc;
 
         // one kernel for both products that read G.  The piece's part of dH first, while the weight's piece is still in L2 from

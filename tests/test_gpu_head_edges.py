@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2512_16273_b200 import tslt
-from test_gpu_head import BF16, F32, gen, loss_case, loss_reference, padded, within
+from test_gpu_head import BF16, F32, U32, UBF, gen, loss_case, loss_reference, padded, within
 
 pytestmark = pytest.mark.gpu
 
@@ -43,6 +43,51 @@ def test_linear_ce_backward_derivatives_that_are_not_finite(rows, V, odd):
         dl[~on] = odd
         g = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
         assert torch.equal(g["dhidden"], want["dhidden"]) and torch.equal(g["dweight"], want["dweight"])
+
+
+# ---- confident rows -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("where", ["even", "first", "last"])
+@pytest.mark.parametrize("rows,D", [(1, 2048), (60, 2048), (200, 8192)])
+def test_linear_ce_backward_confident_rows(rows, D, where):
+    """Rows whose target has probability 1 - 1e-2 ... 1 - 1e-6: G there is the small difference p - 1.  `where`: the columns that the logits'
+    magnitude sits in, which decides how much the tensor cores' truncating additions lose."""
+    V = 1000
+    g = gen(rows + D)
+    wide = torch.full((D,), 0.02, device="cuda")
+    if where == "even":
+        wide[:] = 1.0
+    elif where == "first":
+        wide[:D // 16] = 1.0
+    else:
+        wide[-(D // 16):] = 1.0
+    w = torch.randn(V, D, device="cuda", generator=g) * wide
+    w = (w / w.norm(dim=1, keepdim=True)).to(BF16)
+    t = torch.randperm(V, device="cuda", generator=g)[:rows].to(torch.int32)
+    h = (w[t.long()].float() * torch.linspace(22.0, 12.0, rows, device="cuda")[:, None]).to(BF16)
+    dl = torch.full((rows,), 0.5, device="cuda")
+    hd, wd, tt = h.double(), w.double(), t.long()[:, None]
+    z = hd @ wd.T
+    lse = torch.logsumexp(z, 1)
+    f = tslt.linear_ce(h, w, t)
+    loss = lse - z.gather(1, tt)[:, 0]
+    assert float(loss.min()) < 1e-4
+    # zt is the same fp32 number on both sides of zt - lse, so what is left of it is lse's own: its rounding (2^-24 relative), that of
+    # log2(e) as an fp32 factor (2^-25), some 16 additions to a sum near 1 (2^-24 each) and the power's 2^-22; the other entries
+    # carry their logits' error, a step of 2^-23 of the magnitudes for each of D / 16 additions and as many again within them
+    E = lse.abs() * 2.0 ** -23 + 2.0 ** -19
+    dz = (hd.abs() @ wd.abs().T) * (D / 8 * 2 * U32) + 2.0 ** -19
+    p = torch.exp(z - lse[:, None])
+    gr = p.clone()
+    gr.scatter_add_(1, tt, torch.full((rows, 1), -1.0, dtype=torch.float64, device="cuda"))
+    others = torch.where(gr > 0, gr * dz, torch.zeros_like(gr))
+    gap = others.sum(1) + E  # error of 1 - p, and of a target's entry
+    within(f["loss"], loss, gap + loss * 2 * U32, "loss")
+    dg = UBF * gr.abs() + torch.where(gr > 0, gr * (dz + gap[:, None]), torch.zeros_like(gr))
+    dg.scatter_add_(1, tt, gap[:, None])
+    o = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+    for k, want, bound in (("dhidden", gr @ wd, (dg + (V + 64) * 2 * U32 * gr.abs()) @ wd.abs()),
+                           ("dweight", gr.T @ hd, (dg + (rows + 64) * 2 * U32 * gr.abs()).T @ hd.abs())):
+        within(o[k], 0.5 * want, 0.5 * bound * (1 + UBF) + UBF * 0.5 * want.abs() + 1e-38, k)
 
 
 # ---- copies out of every tile -----------------------------------------------------------------------------------
