@@ -52,6 +52,12 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
+// The largest of |a|, |b| and |c|; a NaN among them is the result (fmaxf drops it).
+__device__ __forceinline__ float top3(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {  // lo in the low half
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
@@ -171,8 +177,10 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * 
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         to_pairs<T>(xv[j], v[j]);
+        if (kNorm) {
 #pragma unroll
-        for (int i = 0; i < P / 2; ++i) squares = fma2(v[j][i], kNorm ? v[j][i] : pair(0.f, 0.f), squares);  // (quantiser: a NaN or infinity shows)
+            for (int i = 0; i < P / 2; ++i) squares = fma2(v[j][i], v[j][i], squares);
+        }
         if (kNorm && p.w) {
             Pair w[P / 2];
             to_pairs<T>(wv[j], w);
@@ -180,11 +188,10 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * 
             for (int i = 0; i < P / 2; ++i) v[j][i] = mul2(v[j][i], w[i]);
         }
 #pragma unroll
-        for (int i = 0; i < P / 2; ++i) top = fmaxf(top, fmaxf(fabsf(lo_of(v[j][i])), fabsf(hi_of(v[j][i]))));
+        for (int i = 0; i < P / 2; ++i) top = top3(top, lo_of(v[j][i]), hi_of(v[j][i]));
     }
-    float sum = lo_of(squares) + hi_of(squares);
-    sum = warp_sum(sum);
-    top = warp_max(top);
+    float sum = kNorm ? warp_sum(lo_of(squares) + hi_of(squares)) : 0.f;
+    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));  // not negative: ordered as integers, a NaN above all
     if (!kWarpRow) {
         if ((tid & 31) == 0) {
             s_sum[tid >> 5] = sum;
@@ -195,12 +202,12 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * 
         top = 0.f;
         for (int w = 0; w < nwarps; ++w) {  // the same order in every thread
             sum += s_sum[w];
-            top = fmaxf(top, s_top[w]);
+            top = top3(top, s_top[w], 0.f);
         }
     }
     float s = top / 127.f;
-    if (kNorm) s = top == 0.f && sum == sum ? 0.f : s / sqrtf(sum / (float)p.D + p.eps);
-    else s += sum;
+    if (kNorm) s = top == 0.f ? 0.f : s / sqrtf(sum / (float)p.D + p.eps);
+    if (!(top < INFINITY)) s = NAN;  // a NaN or an infinity in the row (top is one whatever the weight) or in the weight
     if (tid == 0) p.scale[row] = s;
     const float inv = top > 0.f ? 127.f / top : 0.f;
     // a row with a NaN or an infinity in it, or so small that inv overflows, takes the fp64 quotient throughout

@@ -90,6 +90,26 @@ def test_linear_ce_backward_confident_rows(rows, D, where):
         within(o[k], 0.5 * want, 0.5 * bound * (1 + UBF) + UBF * 0.5 * want.abs() + 1e-38, k)
 
 
+# ---- norm: weights and rows that are not finite ---------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,D", [(1, 100), (3, 4096), (300, 64), (300, 1000), (300, 2500), (300, 5000), (2, 16384)])
+def test_rmsnorm_quant_not_finite(rows, D, dtype):
+    """A NaN or an infinity in the weight gives every row a scale that is NaN; one in a row gives that row's, whatever the weight."""
+    g = gen(rows + D)
+    x = torch.randn(rows, D, device="cuda", generator=g).to(dtype)
+    w = (1 + 0.2 * torch.randn(D, device="cuda", generator=g)).to(dtype)
+    x = padded(x)
+    for odd in (float("nan"), float("inf"), -float("inf")):
+        for at in (0, D - 1):
+            v = w.clone()
+            v[at] = odd
+            assert tslt.rmsnorm_quant(x, v)["scale"].isnan().all()
+            y, v = x.clone(), w.clone()
+            y[0, at], v[at] = odd, 0.0  # the weight hides the column
+            good, bad = tslt.rmsnorm_quant(padded(x.clone()), v), tslt.rmsnorm_quant(padded(y), v)
+            assert bad["scale"][0].isnan() and torch.equal(bad["scale"][1:], good["scale"][1:]) and torch.equal(bad["q"][1:], good["q"][1:])
+
+
 # ---- copies out of every tile -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("logits", [F32, BF16])
 @pytest.mark.parametrize("rows,V", [(640, 128001), (385, 100007), (200, 64 * 1501 + 1), (161, 32 * 3001 + 3), (300, 50000)])
