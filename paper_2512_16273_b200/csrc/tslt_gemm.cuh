@@ -538,7 +538,8 @@ inline uint32_t instruction_desc(bool int8, int m, int n, bool a_mn, bool b_mn) 
 
 // A kernel that waits for the one before it on the stream itself (wait_for_primary_kernel() before it touches global memory), so
 // that its launch and set-up overlap that kernel's end, whatever kernel that is: one that never allows dependents early
-// simply ends first.
+// simply ends first.  Whatever such a kernel reads may have been written during its own life, by the kernel before it: its loads are
+// plain ones, none through the path for data that nobody writes meanwhile.
 template <typename... Params, typename... Args>
 cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
     cudaLaunchConfig_t cfg = {};

@@ -36,12 +36,12 @@ template <typename T> struct HeadEpilogue {
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int v, int lane, int part, gemm::WarpSmem&) {
         const bool on = v < p.V;
-        const float wv = on ? __ldg(p.weight_scale + v) : 0.f;
+        const float wv = on ? p.weight_scale[v] : 0.f;
         const int n = min(t.nt, p.rows - t.col0);
         for (int c = part * 32; c < n; c += kParts * 32) {
             uint32_t r[32];
             gemm::tmem_ld32(tmem + c, r);
-            const float mine = c + lane < n ? __ldg(p.row_scale + t.col0 + c + lane) : 0.f;  // lane j: the scale of column c + j
+            const float mine = c + lane < n ? p.row_scale[t.col0 + c + lane] : 0.f;  // lane j: the scale of column c + j
             gemm::tmem_wait32(r);
             T* out = p.out + (long long)(t.col0 + c) * p.stride + v;
 #pragma unroll
@@ -68,7 +68,7 @@ template <typename T> struct HeadRowsEpilogue {
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part,
                                                gemm::WarpSmem& own) {
-        const float scale = row < p.n_rows ? __ldg(p.row_scale + row) : 0.f;
+        const float scale = row < p.n_rows ? p.row_scale[row] : 0.f;
         constexpr int kStep = 16 / sizeof(T);
         const int whole = p.V / kStep * kStep;
         for (int c = part * kCols; c < t.nt && t.col0 + c < p.V; c += kParts * kCols) {
@@ -77,7 +77,7 @@ template <typename T> struct HeadRowsEpilogue {
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < kCols; i += 32) {
-                const float w = v0 + i + lane < p.V ? __ldg(p.weight_scale + v0 + i + lane) : 0.f;
+                const float w = v0 + i + lane < p.V ? p.weight_scale[v0 + i + lane] : 0.f;
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(own.scratch + 4 * (i + lane)), "f"(w) : "memory");
             }
             __syncwarp();
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kVecThreads, 4) head_vec_kernel(const __grid_c
         const int r = lane / kVecBlock;
         const long long v = v0 + lane % kVecBlock;
         if (r < kRows && r < p.rows && v < p.V) {
-            const float z = (float)mine * __ldg(p.row_scale + r) * __ldg(p.weight_scale + v);
+            const float z = (float)mine * p.row_scale[r] * p.weight_scale[v];
             HeadEpilogue<T>::put(reinterpret_cast<T*>(p.out) + r * p.out_stride + v, z);
         }
     }

@@ -132,7 +132,7 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float acc)
 }
 // The vector of elements [8 i, 8 i + 8) of a row of D, zeros past its end.
 __device__ __forceinline__ uint4 row_vec(const uint16_t* row, int i, int D) {
-    if (8 * i + 8 <= D) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+    if (8 * i + 8 <= D) return reinterpret_cast<const uint4*>(row)[i];
     uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
     }
     // the loads of a warp's first row are in flight while the targets are counted (an ignored row's are thrown away)
     const int vecs = (int)(p.s.ds / 8), row1 = first + warp;
-    const int t1 = row1 < last ? __ldg(p.target + row1) : -1;
+    const int t1 = row1 < last ? p.target[row1] : -1;
     uint4 v[4], u[4];
     auto load = [&](const uint16_t* h, const uint16_t* w, int i0) {
 #pragma unroll
@@ -171,13 +171,13 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
     float top = 0.f;
 #pragma unroll 8
     for (int i = tid; i < p.rows; i += kGatherThreads) {
-        const int t = __ldg(p.target + i);
+        const int t = p.target[i];
         const int c = counts(t, p.V);
         bad |= t >= p.V;
         all += c;
         before += i < first ? c : 0;
         if (p.weight_in && c) {
-            const float g = fabsf(__ldg(p.weight_in + i));
+            const float g = fabsf(p.weight_in[i]);
             if (g < INFINITY) top = fmaxf(top, g);  // a NaN or an infinity stays in its own row
         }
     }
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kGatherThreads) ce_gather_kernel(const __grid_
     }
     int at0 = s_before;
     for (int r0 = first; r0 < last; r0 += 32) {  // 32 rows: a ballot gives each its place
-        const int mine = r0 + lane < last ? __ldg(p.target + r0 + lane) : -1;
+        const int mine = r0 + lane < last ? p.target[r0 + lane] : -1;
         const uint32_t on = __ballot_sync(0xffffffffu, counts(mine, p.V));
         for (int j = warp; j < 32 && r0 + j < last; j += kGatherThreads / 32) {
             const int row = r0 + j, t = __shfl_sync(0xffffffffu, mine, j);
@@ -308,10 +308,10 @@ struct StatsEpilogue {
         // The target's logit is known better than the tensor cores sum it, and it is often most of the row's sum: put the
         // better value in its place.
         const bool on = row < t.rows;
-        const int col = on ? __ldg(p.target + row) - t.col0 : -1;
+        const int col = on ? p.target[row] - t.col0 : -1;
         const bool here = col >= 0 && col < n && (col / 32) % kParts == part;
         const float z = pick_column(tmem, here ? col : -1, lane);
-        if (here) s += ex2_approx(fmaf(__ldg(p.ztarget + row), kLog2e, -m)) - ex2_approx(fmaf(z, p.log2e, -m));
+        if (here) s += ex2_approx(fmaf(p.ztarget[row], kLog2e, -m)) - ex2_approx(fmaf(z, p.log2e, -m));
         if (on) p.part[((long long)t.n * kParts + part) * p.rows_pad + row] = make_float2(m, s);
     }
 };
@@ -329,8 +329,8 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and t
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool, const gemm::Tile& t, int row, int lane, int part, gemm::WarpSmem&) {
         const bool on = row < t.rows;
-        const float lse2 = on ? __ldg(p.lse2 + row) : 0.f, w = on ? __ldg(p.weight + row) : 0.f;
-        const int col = on ? __ldg(p.target + row) - p.v0 - t.col0 : -1;
+        const float lse2 = on ? p.lse2[row] : 0.f, w = on ? p.weight[row] : 0.f;
+        const int col = on ? p.target[row] - p.v0 - t.col0 : -1;
         const int n = min(t.nt, p.n_real - t.col0);  // its last columns, up to a multiple of 64, are zeros
         auto at = [&](int c) { return p.g + ((long long)((t.col0 + c) >> 6) * p.rows_pad + row) * 64 + ((t.col0 + c) & 63); };
         const int end = min(t.nt, (p.n_real + 63) / 64 * 64 - t.col0);
@@ -357,7 +357,7 @@ struct GradEpilogue {  // G of a piece, bf16; zeros in the rows of a tile, and t
         const bool here = col >= 0 && col < n && (col / 32) % kParts == part;
         if (here) {
             uint16_t b;
-            asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"(__ldg(p.gtarget + row)));
+            asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(b) : "f"(p.gtarget[row]));
             *at(col) = b;
         }
     }
@@ -377,7 +377,7 @@ struct WeightEpilogue {
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int lane, int part,
                                                gemm::WarpSmem& own) {
-        const float scale = __ldg(p.scale);
+        const float scale = *p.scale;
         for (int c = part * 64; c < t.nt && t.col0 + c < p.D; c += kParts * 64) {
             uint32_t r[32], b[32];
 #pragma unroll
@@ -453,8 +453,8 @@ struct HiddenRowsEpilogue {  // dH itself, where one tile sums a row's whole gra
     template <int kParts>
     static __device__ __forceinline__ void run(const Params& p, uint32_t tmem, bool zero, const gemm::Tile& t, int row, int, int part, gemm::WarpSmem&) {
         const bool on = row < t.rows;
-        const float scale = __ldg(p.scale);
-        uint16_t* out = p.out + (on ? __ldg(p.row_of + row) : 0) * p.stride;
+        const float scale = *p.scale;
+        uint16_t* out = p.out + (on ? p.row_of[row] : 0) * p.stride;
         for (int c = part * 32; c < t.nt && t.col0 + c < p.D; c += kParts * 32) {
             uint32_t r[32], b[16];
             gemm::tmem_ld32(tmem + c, r);

@@ -115,10 +115,15 @@ template <typename T> __device__ __forceinline__ uint4 load_elems(const void* ro
     constexpr int P = Elt<T>::kPerVec;
     const char* p = (const char*)row + (size_t)at * Elt<T>::kBytes;
     if (at + P <= D) return *reinterpret_cast<const uint4*>(p);
-    float z[P];
+    uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < P; ++i) z[i] = at + i < D ? Elt<T>::load(row, at + i) : 0.f;
-    return pack_vec<T>(z);
+    for (int i = 0; i < P; ++i) {
+        if (at + i < D) {
+            if (Elt<T>::kBytes == 4) w[i & 3] = reinterpret_cast<const uint32_t*>(p)[i];
+            else w[(i / 2) & 3] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T> __device__ __forceinline__ void store_elems(void* row, int at, int D, const uint4& v) {
     constexpr int P = Elt<T>::kPerVec;
