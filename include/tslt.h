@@ -372,8 +372,7 @@ int tslt_diagnostics(const void* draft_logits, const void* target_logits, int dt
  *   v = h * weight (fp32; weight may be NULL: 1), y = v / sqrt(mean(h^2) + eps);
  *   scale = max|y| / 127, q = rint(127 v / max|v|) in [-127, 127], ties to even, so that y ~ q * scale.
  * A row of zeros gives q = 0, scale = 0; a row with a NaN or an infinity, in h or (every row then) in the weight, gives a scale
- * that is NaN, and so does a product h * weight above fp32's range.  (Sums of squares are
- * held in fp32: elements above about 1e17 overflow them, and the scale of such a row is 0.)
+ * that is NaN, and so does a product h * weight above fp32's range.
  * x, residual, weight and residual_out are TSLT_F32 or TSLT_BF16, all the same; residual and residual_out (which gets h) are
  * nullable; residual_out may be x or residual itself (same pointer and stride), no other overlap is allowed.  values
  * (nullable, bf16) gets q * scale, the rows that the codes stand for, for layers that are not held in 8 bits.

@@ -12,7 +12,7 @@
 // Rounding.  t = v * (127 / max|v|) in fp32 is off by at most 1.5 * 2^-23 * 127 = 2.3e-5; where t lies within 1e-4 of
 // the border between two codes (one element in 5000), the code is taken from the quotient in fp64 instead, so that
 // every code is the nearest one to the exact quotient of the fp32 values v and max|v|.  (For bf16 h and w the product
-// v is exact.)
+// v is exact.)  Rows whose sum of squares leaves fp32's range take it in fp64, from a second reading of the row.
 #include "tslt_gemm.cuh"
 
 namespace tslt {
@@ -142,6 +142,24 @@ template <typename T> __device__ __forceinline__ void store_elems(void* row, int
     }
 }
 
+// The sum of squares of h over vectors t, t + nth, ... of a row, in fp64: for rows whose fp32 sum overflows or loses its small squares.
+// h is read again, from where this thread stored it or from x and r.
+template <typename T> __device__ __noinline__ double far_squares(const NormParams& p, long long row, int t, int nth) {
+    constexpr int P = Elt<T>::kPerVec;
+    const char* x = p.h ? (const char*)p.h + row * p.hs * Elt<T>::kBytes : (const char*)p.x + row * p.xs * Elt<T>::kBytes;
+    const char* r = !p.h && p.r ? (const char*)p.r + row * p.rs * Elt<T>::kBytes : nullptr;
+    double sum = 0.0;
+    for (int at = t * P; at < p.D; at += nth * P) {
+        uint4 h = load_elems<T>(x, at, p.D);
+        if (r) h = add_vec<T>(h, load_elems<T>(r, at, p.D));
+        Pair z[P / 2];
+        to_pairs<T>(h, z);
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) sum += (double)lo_of(z[i]) * lo_of(z[i]) + (double)hi_of(z[i]) * hi_of(z[i]);
+    }
+    return warp_sum(sum);
+}
+
 // A row is a CTA's, or (kWarpRow, narrow rows) a warp's with nothing to meet for; thread t of it holds vectors t, t + nthreads, ... (NV of them).
 template <typename T, int NV, bool kNorm, bool kWarpRow>
 __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * Elt<T>::kPerVec == 32 ? 2 : 0) norm_quant_kernel(const __grid_constant__ NormParams p) {
@@ -211,12 +229,27 @@ __global__ void __launch_bounds__(NV * Elt<T>::kPerVec == 32 ? 512 : 1024, NV * 
         }
     }
     float s = top / 127.f;
-    if (kNorm) s = top == 0.f ? 0.f : s / sqrtf(sum / (float)p.D + p.eps);
+    if (kNorm) {
+        const float mean = sum / (float)p.D + p.eps;
+        s = top == 0.f ? 0.f : s / sqrtf(mean);
+        // below 2^-100 the squares that fp32 rounds to steps of 2^-149 could count (the same in every thread of the row)
+        if (top > 0.f && top < INFINITY && !(mean >= 0x1p-100f && mean < INFINITY)) {
+            double all = far_squares<T>(p, row, tid, nth);
+            if (!kWarpRow) {
+                __shared__ double s_far[32];
+                if ((tid & 31) == 0) s_far[tid >> 5] = all;
+                __syncthreads();
+                all = 0.0;
+                for (int w = 0; w < nwarps; ++w) all += s_far[w];
+            }
+            s = (float)((double)top / 127.0 / sqrt(all / p.D + (double)p.eps));
+        }
+    }
     if (!(top < INFINITY)) s = NAN;  // a NaN or an infinity in the row (top is one whatever the weight) or in the weight
     if (tid == 0) p.scale[row] = s;
     const float inv = top > 0.f ? 127.f / top : 0.f;
-    // a row with a NaN or an infinity in it, or so small that inv overflows, takes the fp64 quotient throughout
-    const bool odd = !(inv < 3e38f) || !(top < 3e38f) || !(sum - sum == 0.f);
+    // a row with a NaN or an infinity in it, or so large or small that inv leaves the range, takes the fp64 quotient throughout
+    const bool odd = !(inv < 3e38f) || !(top < 3e38f);
     int8_t* q = p.q + row * p.qs;
     const Pair inv2 = pair(inv, inv), up = pair(kRounder, kRounder), down = pair(-kRounder, -kRounder), minus = pair(-1.f, -1.f), s2 = pair(s, s);
 #pragma unroll

@@ -110,6 +110,28 @@ def test_rmsnorm_quant_not_finite(rows, D, dtype):
             assert bad["scale"][0].isnan() and torch.equal(bad["scale"][1:], good["scale"][1:]) and torch.equal(bad["q"][1:], good["q"][1:])
 
 
+# ---- norm: sums of squares outside fp32's range ---------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,D", [(1, 40), (5, 4096), (300, 100), (300, 2600), (2, 16384)])
+@pytest.mark.parametrize("size", [3e38, 1e25, 1e19, 1e-18, 1e-21, 1e-30, 1e-37])
+@pytest.mark.parametrize("residual", [False, True])
+def test_rmsnorm_quant_sums_of_squares_outside_the_range(rows, D, dtype, size, residual):
+    g = gen(rows + D)
+    x = ((2 * torch.rand(rows, D, device="cuda", generator=g, dtype=torch.float64) - 1) * size * (0.49 if residual else 1)).to(dtype)
+    r = ((2 * torch.rand(rows, D, device="cuda", generator=g, dtype=torch.float64) - 1) * size * 0.49).to(dtype) if residual else None
+    w = (0.5 + 0.4 * torch.rand(D, device="cuda", generator=g)).to(dtype)
+    for eps in (0.0, 1e-6):
+        h = x if r is None else (x.double() + r.double()).to(dtype)
+        v = (h.double() * w.double()).to(F32).double()
+        top = v.abs().amax(1)
+        scale = top / 127 / torch.sqrt((h.double() ** 2).mean(1) + eps)
+        xp, rp = padded(x), None if r is None else padded(r)
+        o = tslt.rmsnorm_quant(xp, w, rp, eps, out={"residual": xp} if residual else None)
+        # fp32 sum and roundings as elsewhere; below 2^-126 the scale itself has steps of 2^-149
+        within(o["scale"], scale, scale * ((D / 2 + 8) * U32) + 2.0 ** -148, "scale")
+        assert torch.equal(o["q"].double(), torch.round(127 * v / top[:, None]))
+
+
 # ---- copies out of every tile -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("logits", [F32, BF16])
 @pytest.mark.parametrize("rows,V", [(640, 128001), (385, 100007), (200, 64 * 1501 + 1), (161, 32 * 3001 + 3), (300, 50000)])
