@@ -34,8 +34,9 @@
  *     row's streaming CTAs in tslt_sparsify) is one-way and bounded: when it runs out, the CTA
  *     sets TSLT_STATUS_WAIT_FELL_BACK in the status word and waits for the end of the streaming
  *     kernel instead; the results are the same.  The first word of the workspace is that device
- *     status word (0 = nothing to report; every call's first kernel clears it), which
- *     tslt_workspace_status reads back; a non-zero word is reported as TSLT_ERR_DEVICE_STATUS.
+ *     status word (0 = nothing to report; every call's first kernel clears it; a call on an empty
+ *     batch launches none and leaves it as it is), which tslt_workspace_status reads back; a
+ *     non-zero word is reported as TSLT_ERR_DEVICE_STATUS.
  */
 #ifndef TSLT_H_
 #define TSLT_H_

@@ -218,6 +218,14 @@ def workspace(nbytes: int, device) -> torch.Tensor:
     return ws
 
 
+def _with_workspace(o: dict, ws: torch.Tensor, rows: int) -> dict:
+    """The outputs with the workspace that holds the call's status word.  An empty batch launches no kernel that would clear it."""
+    if rows == 0:
+        ws[:4].zero_()
+    o["workspace"] = ws
+    return o
+
+
 def sparsify_workspace_bytes(rows: int, V: int, k: int, num_samples: int) -> int:
     n = ctypes.c_size_t(0)
     _check(lib().tslt_sparsify_workspace_bytes(rows, V, k, num_samples, ctypes.byref(n)),
@@ -297,8 +305,7 @@ def sparsify(logits: torch.Tensor, k: int, top_p: float = 1.0, temperature: floa
                              _ptr(o["token"]), _ptr(o.get("lse")), _ptr(o.get("mass")), _ptr(ws),
                              ws.numel(), _stream())
     _check(rc, "tslt_sparsify")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)
 
 
 MAX_SHARDS = 16
@@ -328,8 +335,7 @@ def sparsify_shard(logits_shard: torch.Tensor, k: int, temperature: float = 1.0,
                                    _ptr(o["idx"]), _ptr(o["logit"]), _ptr(o["count"]), _ptr(o["lse2"]), _ptr(ws),
                                    ws.numel(), _stream())
     _check(rc, "tslt_sparsify_shard")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)
 
 
 def sparsify_merge(part_idx: torch.Tensor, part_logit: torch.Tensor, part_count: torch.Tensor,
@@ -381,8 +387,7 @@ def sparsify_merge(part_idx: torch.Tensor, part_logit: torch.Tensor, part_count:
                                    _ptr(o["logit"]), _ptr(o["count"]), _ptr(o["token"]), _ptr(o.get("lse")),
                                    _ptr(o.get("mass")), _ptr(ws), ws.numel(), _stream())
     _check(rc, "tslt_sparsify_merge")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)
 
 
 def sparsify_sharded(logits: torch.Tensor, shard_bounds: Sequence[int], k: int, top_p: float = 1.0,
@@ -470,8 +475,7 @@ def verify(target_logits: torch.Tensor, draft_idx: torch.Tensor, draft_logit: to
                            _ptr(o["accepted_len"]), _ptr(o["out_token"]), _ptr(o.get("accept_prob")),
                            _ptr(o.get("beta_hat")), _ptr(o.get("lse_p")), _ptr(ws), ws.numel(), _stream())
     _check(rc, "tslt_verify")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, B)
 
 
 def verify_static(target_logits: torch.Tensor, draft_idx: torch.Tensor, draft_logit: torch.Tensor,
@@ -563,8 +567,7 @@ def tree_verify(target_logits: torch.Tensor, parent: Sequence[int], node_draft_r
                                 max_depth, _ptr(o["accepted_path"]), _ptr(o["accepted_len"]),
                                 _ptr(o["out_token"]), _ptr(ws), ws.numel(), _stream())
     _check(rc, "tslt_tree_verify_walk" if walk else "tslt_tree_verify")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, B)
 
 
 def verify_packed(target_logits: torch.Tensor, payload: torch.Tensor, prob_format: int, k: int,
@@ -606,8 +609,7 @@ def verify_packed(target_logits: torch.Tensor, payload: torch.Tensor, prob_forma
                                   _ptr(o.get("accept_prob")), _ptr(o.get("beta_hat")), _ptr(o.get("lse_p")), _ptr(ws),
                                   ws.numel(), _stream())
     _check(rc, "tslt_verify_packed")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, B)
 
 
 def tree_verify_packed(target_logits: torch.Tensor, parent: Sequence[int], node_draft_row: Sequence[int],
@@ -652,8 +654,7 @@ def tree_verify_packed(target_logits: torch.Tensor, parent: Sequence[int], node_
                                        _ptr(o["accepted_path"]), _ptr(o["accepted_len"]), _ptr(o["out_token"]), _ptr(ws),
                                        ws.numel(), _stream())
     _check(rc, "tslt_tree_verify_packed")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, B)
 
 
 def payload_words(k: int, V: int, prob_format: int):
@@ -727,8 +728,7 @@ def diagnostics(draft_logits: torch.Tensor, target_logits: torch.Tensor, k_list:
                                 _ptr(o["beta_j"]), _ptr(o["z_j"]), _ptr(o["theta"]), _ptr(o["rho"]), _ptr(o["beta_hat_j"]),
                                 _ptr(o["theta_hat"]), _ptr(ws), ws.numel(), _stream())
     _check(rc, "tslt_diagnostics")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)
 
 
 # ---- the output head around the logits ---------------------------------------------------------------------
@@ -983,8 +983,7 @@ def head_logits(q: torch.Tensor, scale: torch.Tensor, weight: torch.Tensor, weig
     _check(lib().tslt_head_logits(_at(q), _at(scale), qs, _at(weight), _at(weight_scale), wstride, rows, V, D,
                                   F32 if logits_dtype == torch.float32 else BF16, _at(z), zs, _at(ws), ws.numel(), _stream_on(dev)),
            "tslt_head_logits")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)
 
 
 @_own_device
@@ -1053,8 +1052,7 @@ def linear_ce(hidden: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, 
     ws = _space(ws, _loss_workspace_bytes("tslt_linear_ce_workspace_bytes", rows, V, D), device, dev)
     _check(lib().tslt_linear_ce(hidden.data_ptr(), hs, weight.data_ptr(), wstride, target.data_ptr(), rows, V, D, loss.data_ptr(),
                                 lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(dev)), "tslt_linear_ce")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)
 
 
 @_own_device
@@ -1084,5 +1082,4 @@ def linear_ce_backward(hidden: torch.Tensor, weight: torch.Tensor, target: torch
     _check(lib().tslt_linear_ce_backward(hidden.data_ptr(), hs, weight.data_ptr(), wstride, target.data_ptr(), lse.data_ptr(), _at(dloss),
                                          rows, V, D, dh.data_ptr(), dhs, dw.data_ptr(), dws, ws.data_ptr(), ws.numel(), _stream_on(dev)),
            "tslt_linear_ce_backward")
-    o["workspace"] = ws
-    return o
+    return _with_workspace(o, ws, rows)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2512_16273_b200 import tslt
-from test_gpu_head import BF16, F32, U32, UBF, gen, loss_case, loss_reference, padded, within
+from test_gpu_head import BF16, F32, U32, UBF, gen, head_case, loss_case, loss_reference, padded, within
 
 pytestmark = pytest.mark.gpu
 
@@ -130,6 +130,35 @@ def test_rmsnorm_quant_sums_of_squares_outside_the_range(rows, D, dtype, size, r
         # fp32 sum and roundings as elsewhere; below 2^-126 the scale itself has steps of 2^-149
         within(o["scale"], scale, scale * ((D / 2 + 8) * U32) + 2.0 ** -148, "scale")
         assert torch.equal(o["q"].double(), torch.round(127 * v / top[:, None]))
+
+
+# ---- empty batches ----------------------------------------------------------------------------------------------
+def test_status_word_of_an_empty_batch():
+    h, w, t, _ = loss_case(4, 50, 64, 0.0, 1)
+    q, c, s, k, _ = head_case(4, 50, 64, 1)
+
+    def old():
+        return torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")
+    for give in (lambda: None, old):
+        f = tslt.linear_ce(h[:0], w, t[:0], ws=give())
+        b = tslt.linear_ce_backward(h[:0], w, t[:0], f["lse"], ws=give())
+        z = tslt.head_logits(q[:0], s[:0], c, k, ws=give())
+        assert [tslt.workspace_status(o["workspace"]) for o in (f, b, z)] == [0, 0, 0]
+        assert not b["dweight"].any()
+
+
+def test_status_word_of_an_empty_batch_of_logits():
+    V, k = 64, 4
+    z = torch.zeros(0, V, device="cuda")
+    i = torch.zeros(0, k, dtype=torch.int32, device="cuda")
+    f = torch.zeros(0, device="cuda")
+    d = (i, torch.zeros(0, k, device="cuda"), i[:, 0].contiguous())
+    par, ndr = [-1, 0], [0, -1]
+    for ws in (lambda: None, lambda: torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda")):
+        for o in (tslt.sparsify(z, k, ws=ws()), tslt.sparsify_shard(z, k, ws=ws()),
+                  tslt.verify(z.view(0, 2, V), *d, d[2], 1.0, 1.0, f, f, ws=ws()),
+                  tslt.tree_verify(z.view(0, 2, V), par, ndr, d[2], *d, 1.0, 1.0, f, f, 2, ws=ws())):
+            assert tslt.workspace_status(o["workspace"]) == 0
 
 
 # ---- copies out of every tile -----------------------------------------------------------------------------------
