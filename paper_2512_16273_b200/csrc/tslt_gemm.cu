@@ -21,9 +21,20 @@ static EncodeFn encoder() {
 static bool encode(CUtensorMap* map, Element e, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     const EncodeFn fn = encoder();
     const cuuint32_t step[3] = {1, 1, 1};
-    return fn && fn(map, e == kElemInt8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : e == kElemBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, rank, const_cast<void*>(base), dims, strides,
-                    box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const CUtensorMapDataType type = e == kElemInt8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : e == kElemBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    const auto once = [&] {
+        return fn(map, type, rank, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    if (!fn) return false;
+    CUresult r = once();
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+        // a thread that has used the device through nothing that binds its context yet: the driver's calls do not bind it themselves
+        int dev = -1;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
+        r = once();
+    }
+    return r == CUDA_SUCCESS;
 }
 
 bool encode_map(CUtensorMap* map, Element e, const void* base, long long inner, long long outer, long long row_bytes, int box_outer) {

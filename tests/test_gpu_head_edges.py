@@ -1,6 +1,8 @@
 """GPU tests of the output head's calls at their edges, against their definitions in 64 bits.
 
 Tolerances count roundings as test_gpu_head.py does: finfo(type).eps / 2 relative for one rounding."""
+import threading
+
 import pytest
 import torch
 
@@ -130,6 +132,29 @@ def test_rmsnorm_quant_sums_of_squares_outside_the_range(rows, D, dtype, size, r
         # fp32 sum and roundings as elsewhere; below 2^-126 the scale itself has steps of 2^-149
         within(o["scale"], scale, scale * ((D / 2 + 8) * U32) + 2.0 ** -148, "scale")
         assert torch.equal(o["q"].double(), torch.round(127 * v / top[:, None]))
+
+
+# ---- a thread's first call ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("name", ["norm", "head of 3 rows", "head of 20 rows", "head of 300 rows", "loss", "gradients"])
+def test_first_call_of_a_thread(name, given):
+    """A thread whose first use of the device is the call itself, with a workspace given or not."""
+    h, w, t, dl = loss_case(90, 500, 64, 0.0, 3)
+    q, c, s, k, _ = head_case(300, 500, 64, 1)
+    f = tslt.linear_ce(h, w, t)
+    ws = torch.empty(tslt.linear_ce_backward_workspace_bytes(90, 500, 64), dtype=torch.uint8, device="cuda") if given else None
+    call = {"norm": lambda: tslt.rmsnorm_quant(h)["q"], "head of 3 rows": lambda: tslt.head_logits(q[:3], s[:3], c, k, ws=ws)["logits"],
+            "head of 20 rows": lambda: tslt.head_logits(q[:20], s[:20], c, k, ws=ws)["logits"],
+            "head of 300 rows": lambda: tslt.head_logits(q, s, c, k, ws=ws)["logits"], "loss": lambda: tslt.linear_ce(h, w, t, ws=ws)["loss"],
+            "gradients": lambda: tslt.linear_ce_backward(h, w, t, f["lse"], dl, ws=ws)["dweight"]}[name]
+    want = call().clone()
+    got = []
+    torch.cuda.synchronize()
+    th = threading.Thread(target=lambda: got.append(call()))
+    th.start()
+    th.join()
+    torch.cuda.synchronize()
+    assert len(got) == 1 and torch.equal(got[0], want)
 
 
 # ---- empty batches ----------------------------------------------------------------------------------------------
