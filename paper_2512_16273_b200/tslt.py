@@ -842,20 +842,10 @@ def _stride(t: torch.Tensor, cols: int, name: str) -> int:
     return _matrix(t, "output " + name, None, t.get_device(), cols)[2]
 
 
-_head_ws: Dict[tuple, torch.Tensor] = {}
-
-
 def _scratch(nbytes: int, device) -> torch.Tensor:
-    """A workspace of the current stream's, kept for its next call; under graph capture a buffer of the graph's own, so
-    that two captured graphs never share one."""
-    if torch.cuda.is_current_stream_capturing():
-        return torch.empty(max(int(nbytes), 4096), dtype=torch.uint8, device=device)
-    key = (device.index, _stream_on(device.index))
-    ws = _head_ws.get(key)
-    if ws is None or ws.numel() < nbytes:
-        ws = torch.empty(max(int(nbytes), 4096), dtype=torch.uint8, device=device)
-        _head_ws[key] = ws
-    return ws
+    """A workspace of this call's own, from the current stream's pool (under graph capture the graph's): threads that call on one
+    stream, whose launches may interleave, and captured graphs share none, and its status word stays the call's."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def _space(ws, nbytes: int, device, dev: int) -> torch.Tensor:

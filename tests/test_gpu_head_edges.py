@@ -157,6 +157,57 @@ def test_first_call_of_a_thread(name, given):
     assert len(got) == 1 and torch.equal(got[0], want)
 
 
+# ---- workspaces and status words ------------------------------------------------------------------------------
+def test_status_word_of_a_call_is_its_own():
+    """What a call reports stands in the workspace that it returned, whatever the same stream runs next."""
+    q, w, s, c, _ = head_case(3, 100, 64, 1)
+    h, lw, t, dl = loss_case(20, 100, 64, 0.0, 9)
+    t[3] = 100
+    f = tslt.linear_ce(h, lw, t)
+    b = tslt.linear_ce_backward(h, lw, t, f["lse"])
+    z = tslt.head_logits(q, s, w, c)
+    assert len({o["workspace"].data_ptr() for o in (f, b, z)}) == 3
+    assert tslt.workspace_status(f["workspace"]) == tslt.workspace_status(b["workspace"]) == tslt.STATUS_BAD_TARGET
+    assert tslt.workspace_status(z["workspace"]) == 0
+
+
+def test_workspaces_of_calls_in_flight_are_distinct():
+    """Also when a later call needs less or as much as an earlier one."""
+    h, w, t, dl = loss_case(90, 500, 64, 0.0, 3)
+    f = [tslt.linear_ce(h, w, t) for _ in range(3)]
+    b = [tslt.linear_ce_backward(h, w, t, f[0]["lse"], dl) for _ in range(2)]
+    assert len({o["workspace"].data_ptr() for o in f + b}) == 5
+
+
+def test_threads_on_one_stream():
+    """Threads that call on the same stream do not hand each other's rows over: the results are those of one thread alone."""
+    cases = [loss_case(90, 1500, 256, 0.1 * s, 50 + s) for s in range(4)]
+    want = []
+    for h, w, t, dl in cases:
+        f = tslt.linear_ce(h, w, t)
+        b = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+        want.append([f["loss"], f["lse"], b["dhidden"], b["dweight"]])
+    torch.cuda.synchronize()
+    got = [[] for _ in cases]
+    start = threading.Barrier(len(cases))
+
+    def work(i):
+        h, w, t, dl = cases[i]
+        start.wait()
+        for _ in range(40):
+            f = tslt.linear_ce(h, w, t)
+            b = tslt.linear_ce_backward(h, w, t, f["lse"], dl)
+            got[i].append([f["loss"], f["lse"], b["dhidden"], b["dweight"]])
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert len(a) == 40 and all(torch.equal(x, y) for o in a for x, y in zip(o, b))
+
+
 # ---- empty batches ----------------------------------------------------------------------------------------------
 def test_status_word_of_an_empty_batch():
     h, w, t, _ = loss_case(4, 50, 64, 0.0, 1)
