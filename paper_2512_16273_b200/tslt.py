@@ -205,17 +205,11 @@ def _row_layout(logits: torch.Tensor):
     return rows, V, max(int(stride), V)
 
 
-_ws_cache: Dict[tuple, torch.Tensor] = {}
-
-
 def workspace(nbytes: int, device) -> torch.Tensor:
-    """A cached device buffer of at least nbytes (torch's allocator returns >= 512-byte aligned)."""
-    key = (str(device), torch.cuda.current_stream(device).cuda_stream)
-    ws = _ws_cache.get(key)
-    if ws is None or ws.numel() < nbytes:
-        ws = torch.empty(max(int(nbytes), 4096), dtype=torch.uint8, device=device)
-        _ws_cache[key] = ws
-    return ws
+    """A device buffer of at least nbytes (torch's allocator returns >= 512-byte aligned) for one call, from the current stream's pool
+    (under graph capture the graph's): threads that call on one stream, whose launches may interleave, and captured graphs share
+    none, and its status word stays the call's."""
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
 def _with_workspace(o: dict, ws: torch.Tensor, rows: int) -> dict:
@@ -842,15 +836,9 @@ def _stride(t: torch.Tensor, cols: int, name: str) -> int:
     return _matrix(t, "output " + name, None, t.get_device(), cols)[2]
 
 
-def _scratch(nbytes: int, device) -> torch.Tensor:
-    """A workspace of this call's own, from the current stream's pool (under graph capture the graph's): threads that call on one
-    stream, whose launches may interleave, and captured graphs share none, and its status word stays the call's."""
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
-
-
 def _space(ws, nbytes: int, device, dev: int) -> torch.Tensor:
     if ws is None:
-        return _scratch(nbytes, device)
+        return workspace(nbytes, device)
     _check_tensor(ws, "ws", torch.uint8, dev)
     if not ws.is_contiguous():
         raise ValueError("ws must be contiguous")
@@ -986,8 +974,7 @@ def sparsify_hidden(x: torch.Tensor, norm_weight: Optional[torch.Tensor], head: 
     sparsify.  Returns what sparsify returns, and logits [..., V] and (with a residual) residual [..., D]."""
     n = rmsnorm_quant(x, norm_weight, residual, eps)
     z = head_logits(n["q"], n["scale"], head, head_scale, logits_dtype)["logits"]
-    o = sparsify(z, k, top_p, temperature, uniforms, ws=_scratch(sparsify_workspace_bytes(z.numel() // z.shape[-1], z.shape[-1], k,
-                 0 if uniforms is None else uniforms.numel() // max(1, z.numel() // z.shape[-1])), x.device))
+    o = sparsify(z, k, top_p, temperature, uniforms)
     o["logits"] = z
     if residual is not None:
         o["residual"] = n["residual"]
