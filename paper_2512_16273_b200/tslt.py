@@ -971,11 +971,13 @@ def sparsify_hidden(x: torch.Tensor, norm_weight: Optional[torch.Tensor], head: 
                     logits_dtype: torch.dtype = torch.bfloat16) -> dict:
     """The draft side from the last layer's hidden states on: rmsnorm_quant, head_logits and sparsify, one after the other
     on the current stream.  x, residual [..., D]; head [V, D] int8 and head_scale [V] from quantize_rows; the rest as in
-    sparsify.  Returns what sparsify returns, and logits [..., V] and (with a residual) residual [..., D]."""
+    sparsify.  Returns what sparsify returns, and logits [..., V], head_workspace (the head product's, with its status word) and
+    (with a residual) residual [..., D]."""
     n = rmsnorm_quant(x, norm_weight, residual, eps)
-    z = head_logits(n["q"], n["scale"], head, head_scale, logits_dtype)["logits"]
+    p = head_logits(n["q"], n["scale"], head, head_scale, logits_dtype)
+    z = p["logits"]
     o = sparsify(z, k, top_p, temperature, uniforms)
-    o["logits"] = z
+    o["logits"], o["head_workspace"] = z, p["workspace"]
     if residual is not None:
         o["residual"] = n["residual"]
     return o

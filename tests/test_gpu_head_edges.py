@@ -237,6 +237,17 @@ def test_status_word_of_an_empty_batch_of_logits():
             assert tslt.workspace_status(o["workspace"]) == 0
 
 
+# ---- both status words ------------------------------------------------------------------------------------------
+def test_sparsify_hidden_reports_both_status_words():
+    q, c, s, k, _ = head_case(4, 500, 64, 1)
+    x = torch.randn(4, 64, device="cuda").to(BF16)
+    o = tslt.sparsify_hidden(x, None, c, k, 8)
+    assert o["head_workspace"].data_ptr() != o["workspace"].data_ptr()
+    assert tslt.workspace_status(o["head_workspace"]) == 0 and tslt.workspace_status(o["workspace"]) == 0
+    o["head_workspace"][:4] = torch.tensor([4, 0, 0, 0], dtype=torch.uint8)
+    assert tslt.workspace_status(o["workspace"]) == 0
+
+
 # ---- copies out of every tile -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("logits", [F32, BF16])
 @pytest.mark.parametrize("rows,V", [(640, 128001), (385, 100007), (200, 64 * 1501 + 1), (161, 32 * 3001 + 3), (300, 50000)])
