@@ -128,80 +128,96 @@ struct VecParams {
     int rows, V, K;
     int* status;
 };
+// Weight rows v0 ... v0 + 3 by a warp.  What stands between a row's last code and the next row meets zeros; behind the last row there
+// may be nothing: kEnd, the block that holds it, takes the codes behind its whole chunks one by one.
+template <int kRows, typename T, bool kEnd>
+__device__ __forceinline__ void head_vec_block(const VecParams& p, const uint8_t* s_codes, int chunks, long long v0, int lane) {
+    const uint4* codes = reinterpret_cast<const uint4*>(s_codes);
+    const int whole = kEnd ? p.K / 16 : chunks;
+    int acc[kVecBlock][kRows];
+#pragma unroll
+    for (int b = 0; b < kVecBlock; ++b)
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) acc[b][r] = 0;
+    const int8_t* w[kVecBlock];
+#pragma unroll
+    for (int b = 0; b < kVecBlock; ++b) w[b] = p.w + (v0 + b < p.V ? v0 + b : p.V - 1) * p.w_stride;
+    for (int c0 = lane; c0 < whole; c0 += 64) {  // eight loads in flight
+        uint4 x[2][kVecBlock];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int b = 0; b < kVecBlock; ++b)
+                x[u][b] = c0 + 32 * u < whole ? __ldcs(reinterpret_cast<const uint4*>(w[b]) + c0 + 32 * u) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const uint4 q = codes[r * chunks + (c0 + 32 * u < whole ? c0 + 32 * u : lane)];
+#pragma unroll
+                for (int b = 0; b < kVecBlock; ++b) {
+                    acc[b][r] = __dp4a((int)x[u][b].x, (int)q.x, acc[b][r]);
+                    acc[b][r] = __dp4a((int)x[u][b].y, (int)q.y, acc[b][r]);
+                    acc[b][r] = __dp4a((int)x[u][b].z, (int)q.z, acc[b][r]);
+                    acc[b][r] = __dp4a((int)x[u][b].w, (int)q.w, acc[b][r]);
+                }
+            }
+        }
+    }
+    if (kEnd && whole * 16 + lane < p.K) {  // fewer than 16 codes: one a lane
+#pragma unroll
+        for (int b = 0; b < kVecBlock; ++b) {
+            const int x = w[b][whole * 16 + lane];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) acc[b][r] += x * (int8_t)s_codes[(r * chunks + whole) * 16 + lane];
+        }
+    }
+    // lane 4 r + b ends up with the sum of row r and weight row b
+    int mine = 0;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int b = 0; b < kVecBlock; ++b) {
+            const int sum = __reduce_add_sync(0xffffffffu, acc[b][r]);
+            if (lane == r * kVecBlock + b) mine = sum;
+        }
+    const int r = lane / kVecBlock;
+    const long long v = v0 + lane % kVecBlock;
+    if (r < kRows && r < p.rows && v < p.V) {
+        const float z = (float)mine * p.row_scale[r] * p.weight_scale[v];
+        HeadEpilogue<T>::put(reinterpret_cast<T*>(p.out) + r * p.out_stride + v, z);
+    }
+}
 template <int kRows, typename T>
 __global__ void __launch_bounds__(kVecThreads, 4) head_vec_kernel(const __grid_constant__ VecParams p) {
     extern __shared__ __align__(16) uint8_t s_codes[];
     const int tid = threadIdx.x, lane = tid & 31;
     wait_for_primary_kernel();
     allow_dependent_launch();
-    const int chunks = (p.K + 15) / 16;  // a row's last 16 bytes may hold anything behind K: they meet zeros
+    const int chunks = (p.K + 15) / 16;
     if (blockIdx.x == 0 && tid == 0) *p.status = 0;  // nothing here waits
     for (int i = tid; i < kRows * chunks; i += kVecThreads) {
         const int r = i / chunks, at = (i - r * chunks) * 16;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (r < p.rows) {
-            v = *reinterpret_cast<const uint4*>(p.q + r * p.q_stride + at);
-            if (at + 16 > p.K) {  // zeros behind the last code
-                uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+            const int8_t* q = p.q + r * p.q_stride + at;
+            if (at + 16 <= p.K) {
+                v = *reinterpret_cast<const uint4*>(q);
+            } else {  // zeros behind the last code, and nothing read there: the buffer may end with it
+                uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int n = p.K - at - 4 * j;  // codes left in this word
-                    w[j] = n >= 4 ? w[j] : n <= 0 ? 0u : w[j] & ((1u << (8 * n)) - 1u);
-                }
+                for (int j = 0; j < 15; ++j)
+                    if (at + j < p.K) w[j / 4] |= (uint32_t)(uint8_t)q[j] << (8 * (j % 4));
+                v = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
         reinterpret_cast<uint4*>(s_codes)[i] = v;
     }
     __syncthreads();
-    const uint4* codes = reinterpret_cast<const uint4*>(s_codes);
-    const int warps = gridDim.x * (kVecThreads / 32);
-    for (long long v0 = (long long)(blockIdx.x * (kVecThreads / 32) + (tid >> 5)) * kVecBlock; v0 < p.V; v0 += (long long)warps * kVecBlock) {
-        int acc[kVecBlock][kRows];
-#pragma unroll
-        for (int b = 0; b < kVecBlock; ++b)
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) acc[b][r] = 0;
-        const int8_t* w[kVecBlock];
-#pragma unroll
-        for (int b = 0; b < kVecBlock; ++b) w[b] = p.w + (v0 + b < p.V ? v0 + b : p.V - 1) * p.w_stride;
-        for (int c0 = lane; c0 < chunks; c0 += 64) {  // eight loads in flight
-            uint4 x[2][kVecBlock];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int b = 0; b < kVecBlock; ++b)
-                    x[u][b] = c0 + 32 * u < chunks ? __ldcs(reinterpret_cast<const uint4*>(w[b]) + c0 + 32 * u) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-                    const uint4 q = codes[r * chunks + (c0 + 32 * u < chunks ? c0 + 32 * u : lane)];
-#pragma unroll
-                    for (int b = 0; b < kVecBlock; ++b) {
-                        acc[b][r] = __dp4a((int)x[u][b].x, (int)q.x, acc[b][r]);
-                        acc[b][r] = __dp4a((int)x[u][b].y, (int)q.y, acc[b][r]);
-                        acc[b][r] = __dp4a((int)x[u][b].z, (int)q.z, acc[b][r]);
-                        acc[b][r] = __dp4a((int)x[u][b].w, (int)q.w, acc[b][r]);
-                    }
-                }
-            }
-        }
-        // lane 4 r + b ends up with the sum of row r and weight row b
-        int mine = 0;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r)
-#pragma unroll
-            for (int b = 0; b < kVecBlock; ++b) {
-                const int sum = __reduce_add_sync(0xffffffffu, acc[b][r]);
-                if (lane == r * kVecBlock + b) mine = sum;
-            }
-        const int r = lane / kVecBlock;
-        const long long v = v0 + lane % kVecBlock;
-        if (r < kRows && r < p.rows && v < p.V) {
-            const float z = (float)mine * p.row_scale[r] * p.weight_scale[v];
-            HeadEpilogue<T>::put(reinterpret_cast<T*>(p.out) + r * p.out_stride + v, z);
-        }
-    }
+    const long long step = (long long)gridDim.x * (kVecThreads / 32) * kVecBlock, end = p.K % 16 ? (p.V - 1) / kVecBlock * kVecBlock : p.V;
+    long long v0 = (long long)(blockIdx.x * (kVecThreads / 32) + (tid >> 5)) * kVecBlock;
+    for (; v0 < end; v0 += step) head_vec_block<kRows, T, false>(p, s_codes, chunks, v0, lane);
+    if (v0 < p.V) head_vec_block<kRows, T, true>(p, s_codes, chunks, v0, lane);  // of a ragged K only: the block that starts at `end`
 }
 
 template <int kRows, typename T> static int launch_vec(VecParams p, int* status, cudaStream_t st) {

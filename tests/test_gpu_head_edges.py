@@ -248,6 +248,27 @@ def test_sparsify_hidden_reports_both_status_words():
     assert tslt.workspace_status(o["workspace"]) == 0
 
 
+# ---- buffers of the exact size ----------------------------------------------------------------------------------
+def exact(t, stride):
+    """The rows of t at `stride`, in a buffer that ends with the last row's last element."""
+    n, d = t.shape
+    buf = torch.empty((n - 1) * stride + d, dtype=t.dtype, device="cuda")
+    v = buf.as_strided((n, d), (stride, 1))
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("logits", [F32, BF16])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4])
+@pytest.mark.parametrize("D", [1, 15, 16, 17, 33, 511, 512, 527, 1601, 4090])
+def test_head_logits_rows_that_end_with_their_buffer(rows, D, logits):
+    V = 1003
+    q, w, s, t, want = head_case(rows, V, D, rows + D)
+    st = (D + 15) // 16 * 16
+    z = tslt.head_logits(exact(q, st), s, exact(w, st), t, logits)["logits"]
+    within(z, want, want.abs() * (3 * U32 * 1.01 + (UBF if logits == BF16 else 0)) + 1e-40, "logits")
+
+
 # ---- copies out of every tile -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("logits", [F32, BF16])
 @pytest.mark.parametrize("rows,V", [(640, 128001), (385, 100007), (200, 64 * 1501 + 1), (161, 32 * 3001 + 3), (300, 50000)])
