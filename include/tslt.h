@@ -375,7 +375,7 @@ int tslt_diagnostics(const void* draft_logits, const void* target_logits, int dt
  * A row of zeros gives q = 0, scale = 0; a row with a NaN or an infinity, in h or (every row then) in the weight, gives a scale
  * that is NaN, and so does a product h * weight above fp32's range.
  * x, residual, weight and residual_out are TSLT_F32 or TSLT_BF16, all the same; residual and residual_out (which gets h) are
- * nullable; residual_out may be x or residual itself (same pointer and stride), no other overlap is allowed.  values
+ * nullable; residual_out may be x or residual itself (same pointer and stride; another stride is refused), no other overlap is allowed.  values
  * (nullable, bf16) gets q * scale, the rows that the codes stand for, for layers that are not held in 8 bits.
  * tslt_quantize_rows: the same quantiser without norm and weight (y = x): lays a head weight [V, D] out once for
  * tslt_head_logits, one scale per vocabulary entry.

@@ -686,6 +686,7 @@ extern "C" int tslt_linear_ce(const void* hidden, long long hidden_stride, const
     if (!loss || !lse || !workspace || ((uintptr_t)workspace & 255)) return TSLT_ERR_INVALID_ARG;
     const CeSpace s = ce_space(workspace, rows, V, D, false);
     if (workspace_bytes < s.bytes) return TSLT_ERR_WORKSPACE;
+    if (loss == lse || (const void*)loss == target || (const void*)lse == target) return TSLT_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
     gemm::Product p;
     gemm::Maps maps;

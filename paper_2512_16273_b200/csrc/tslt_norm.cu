@@ -344,6 +344,8 @@ extern "C" int tslt_rmsnorm_quant(const void* x, const void* residual, const voi
     if (!row_ok(x, x_stride, D, b) || !row_ok(q, q_stride, D, 1) || !scale) return TSLT_ERR_INVALID_ARG;
     if (residual && !row_ok(residual, residual_stride, D, b)) return TSLT_ERR_INVALID_ARG;
     if (residual_out && !row_ok(residual_out, out_stride, D, b)) return TSLT_ERR_INVALID_ARG;
+    if (rows > 1 && residual_out && ((residual_out == x && out_stride != x_stride) || (residual_out == residual && out_stride != residual_stride)))
+        return TSLT_ERR_INVALID_ARG;  // a row would go over another that is still to be read
     if (values && !row_ok(values, values_stride, D, 2)) return TSLT_ERR_INVALID_ARG;
     if (weight && !aligned16(weight)) return TSLT_ERR_INVALID_ARG;
     NormParams p = {x, residual, weight, residual_out, (uint16_t*)values, (int8_t*)q, scale, x_stride, residual_stride, out_stride,
