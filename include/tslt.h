@@ -406,6 +406,9 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  * Softmax cross entropy of a linear head, z = hidden weight^T (bf16 operands, fp32 sums), computed in pieces of
  * the vocabulary without keeping the logits:
  *   lse[n] = ln sum_v exp z[n, v],  loss[n] = lse[n] - z[n, target[n]].
+ * The tensor cores' sums lose a little of every logit; what a logit that grows evenly over the D units loses in the mean is put back (a
+ * factor 1 + D 2^-30).  A logit that stands after the first units keeps an error of about -D 2^-30 |z|, one that grows in the last
+ * units, or whose sum is exact, D 2^-30 |z|.  The target's logit is an fp32 dot product of its own.
  * A row with target < 0 is ignored: loss = lse = 0 there, and its hidden row is never used (it may hold anything,
  * NaN included).  target >= V is taken as ignored too and sets TSLT_STATUS_BAD_TARGET.
  * tslt_linear_ce_backward: with dloss[n] the derivative of the caller's total by loss[n] (NULL: 1 everywhere) and

@@ -263,10 +263,13 @@ __device__ __forceinline__ float pick_column(uint32_t tmem, int col, int lane) {
 }
 
 // The tensor cores' fp32 additions truncate: each of the D / 16 that a logit is summed with loses up to 2^-23 of the running
-// sum, which is half the logit in the mean.  So a logit comes out too small by a factor 1 - c D / 16 2^-25, where c = 0.72
-// for half a unit lost at evenly spread mantissas; measured c = 0.52, the same at D = 1000, 2048 and 4096 (the mean error
-// of 77, 2048 and 6144 values of lse: -3.7e-6, -7.3e-6, -1.55e-5).  The factor that makes up for it costs nothing: it goes
-// into log2(e).  What is left of the error is 1e-6 at D = 4096, the fp32 rounding of lse itself.
+// sum, which is half the logit in the mean where the sum grows evenly.  Such a logit comes out too small by a factor
+// 1 - c D / 16 2^-25, where c = 0.72 for half a unit lost at evenly spread mantissas; measured c = 0.51 to 0.55 (D = 512 to 16384;
+// normal, positive and shifted inputs, a hundredth of the units twelve times larger).  The factor that makes up for it costs nothing:
+// it goes into log2(e), for lse and G alike.  It leaves a mean error of lse of 1e-7 relative at D = 4096 and a largest one of 1e-6,
+// which an fp32 product without tensor cores has too.  A sum that is complete after its first columns loses twice as much (c = 1.07),
+// one that grows in its last columns or is exact nothing: there the error is that of no factor at all in size, with the sign turned
+// (3.3e-5 at D = 4096, z = 8).  Without the factor lse would be 0 to 6.8e-5 too small, with it it is off by -3.5e-5 to 3.3e-5.
 static float log2e_for(int D) { return (float)(1.4426950408889634 * (1.0 + (D / 16) * (0.52 / 33554432.0))); }
 
 struct StatsEpilogue {

@@ -1,6 +1,7 @@
 """GPU tests of the output head's calls at their edges, against their definitions in 64 bits.
 
 Tolerances count roundings as test_gpu_head.py does: finfo(type).eps / 2 relative for one rounding."""
+import math
 import threading
 
 import pytest
@@ -300,3 +301,53 @@ def test_linear_ce_backward_copies_of_every_tile(rows, V, D):
             for k in ("dhidden", "dweight"):
                 within(g[k], d[k], b[k], k)
         assert torch.equal(g["dhidden"], first["dhidden"]) and torch.equal(g["dweight"], first["dweight"])
+
+
+# ---- the bias of the tensor cores' sums ---------------------------------------------------------------------------
+def correction(D):
+    """What the loss multiplies a logit by, less 1: D / 16 additions that lose 0.52 units of 2^-25 of it each."""
+    return D // 16 * 0.52 / 2.0 ** 25
+
+
+@pytest.mark.parametrize("where", ["even", "first", "last"])
+@pytest.mark.parametrize("D", [512, 4096, 8192, 16384])
+def test_linear_ce_mean_error_of_lse(D, where):
+    """Sums that grow evenly: the correction leaves less than half of the bias that it is there for.  0.52 is measured; half a unit lost at
+    evenly spread mantissas gives 0.72, so the rest is at most 0.2 / 0.52 of it if either holds.  Sums that stand after their first
+    columns lose twice as much, sums that grow in the last nothing: the correction once more, and the same half.  lse moves by
+    the mean of z under the softmax."""
+    rows, V = 512, 4096
+    g = gen(D)
+    wide = torch.full((D,), 1.0 if where == "even" else 0.02, device="cuda")
+    if where != "even":
+        (wide[:D // 16] if where == "first" else wide[-(D // 16):]).fill_(1.0)
+    h = (torch.randn(rows, D, device="cuda", generator=g) * wide).to(BF16)
+    w = (torch.randn(V, D, device="cuda", generator=g) * (3 / math.sqrt(D) / float((wide ** 2).mean()) ** 0.5)).to(BF16)
+    t = torch.randint(0, V, (rows,), device="cuda", generator=g).to(torch.int32)  # (targets, whose logits are exact, hold little)
+    z = h.double() @ w.double().T
+    lse = torch.logsumexp(z, 1)
+    bias = correction(D) * float((torch.softmax(z, 1) * z).sum(1).mean())
+    err = float((tslt.linear_ce(h, w, t)["lse"].double() - lse).mean())
+    # the roundings of log2(e) (2^-25 relative) and of lse itself and the power's 2^-22, at their largest in the mean
+    rest = 2.0 ** -22 + float(lse.mean()) * 2.0 ** -25 + float(lse.mean()) * 2.0 ** -24 / math.sqrt(rows) * 3
+    assert abs(err) <= (0.5 if where == "even" else 1.5) * bias + rest, (err, bias)
+
+
+@pytest.mark.parametrize("D", [512, 4096, 16384])
+@pytest.mark.parametrize("rows", [40, 300])
+def test_linear_ce_sums_that_are_exact(rows, D):
+    """Hidden rows with one unit that is not zero: the tensor cores lose nothing, so lse is off by the correction and fp32's roundings."""
+    V = 700
+    g = gen(rows + D)
+    w = torch.randint(-24, 25, (V, D), device="cuda", generator=g).to(BF16)
+    h = torch.zeros(rows, D, dtype=BF16, device="cuda")
+    at = torch.randint(0, D, (rows,), device="cuda", generator=g)
+    h[torch.arange(rows, device="cuda"), at] = 1.0
+    t = torch.randint(0, V, (rows,), device="cuda", generator=g).to(torch.int32)
+    z = h.double() @ w.double().T
+    lse = torch.logsumexp(z, 1)
+    f = tslt.linear_ce(h, w, t)
+    # the factor's own rounding to fp32 (2^-24 of a logit at most), lse's rounding, the powers and additions of the sum
+    bound = z.abs().amax(1) * (correction(D) + 2 * U32) + lse.abs() * U32 + 2.0 ** -19
+    within(f["lse"], lse, bound, "lse")
+    within(f["loss"], lse - z.gather(1, t.long()[:, None])[:, 0], bound + (lse.abs() + z.abs().amax(1)) * U32, "loss")
