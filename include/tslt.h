@@ -375,8 +375,8 @@ int tslt_diagnostics(const void* draft_logits, const void* target_logits, int dt
  * A row of zeros gives q = 0, scale = 0; a row with a NaN or an infinity, in h or (every row then) in the weight, gives a scale
  * that is NaN, and so does a product h * weight above fp32's range.
  * x, residual, weight and residual_out are TSLT_F32 or TSLT_BF16, all the same; residual and residual_out (which gets h) are
- * nullable; residual_out may be x or residual itself (same pointer and stride; another stride is refused), no other overlap is allowed.  values
- * (nullable, bf16) gets q * scale, the rows that the codes stand for, for layers that are not held in 8 bits.
+ * nullable; residual_out may be x or residual itself (same pointer and stride; another stride is refused), no other overlap
+ * is allowed.  values (nullable, bf16) gets q * scale, the rows that the codes stand for, for layers that are not held in 8 bits.
  * tslt_quantize_rows: the same quantiser without norm and weight (y = x): lays a head weight [V, D] out once for
  * tslt_head_logits, one scale per vocabulary entry.
  * Rows: x [rows, D] with a stride; q [rows, D] int8 with a stride; scale [rows] fp32.  Every base pointer 16-byte aligned,
@@ -406,9 +406,10 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  * Softmax cross entropy of a linear head, z = hidden weight^T (bf16 operands, fp32 sums), computed in pieces of
  * the vocabulary without keeping the logits:
  *   lse[n] = ln sum_v exp z[n, v],  loss[n] = lse[n] - z[n, target[n]].
- * The tensor cores' sums lose a little of every logit; what a logit that grows evenly over the D units loses in the mean is put back (a
- * factor 1 + D 2^-30).  A logit that stands after the first units keeps an error of about -D 2^-30 |z|, one that grows in the last
- * units, or whose sum is exact, D 2^-30 |z|.  The target's logit is an fp32 dot product of its own.
+ * The tensor cores' sums lose a little of every logit's magnitude; what a logit that grows evenly over the D units loses in
+ * the mean is put back (a factor 1 + D 2^-30).  A logit that stands after the first units stays about D 2^-30 |z| too small,
+ * one that grows in the last units, or whose sum is exact, comes out as much too large.  The target's logit is an fp32 dot
+ * product of its own.
  * A row with target < 0 is ignored: loss = lse = 0 there, and its hidden row is never used (it may hold anything,
  * NaN included).  target >= V is taken as ignored too and sets TSLT_STATUS_BAD_TARGET.
  * tslt_linear_ce_backward: with dloss[n] the derivative of the caller's total by loss[n] (NULL: 1 everywhere) and
@@ -417,10 +418,10 @@ int tslt_head_logits(const signed char* q, const float* q_scale, long long q_str
  * both overwritten whole (zeros for ignored rows; zeros in dweight when no row counts).  lse is what tslt_linear_ce
  * wrote.  A NaN or an infinity in a row that counts, or logits that overflow fp32, make that row's loss, lse and
  * dhidden not finite, and dweight with them; other rows keep theirs.  So does a dloss that is not finite with its row's
- * dhidden and with dweight.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of the outputs'
- * own rounding) and counts as 0 below 2^-126 times the largest finite |dloss|; at a
- * target of probability near 1 it is formed from an fp32 dot product of its own and lse as given, whose fp32 rounding (2^-24 |lse|) then
- * is an error of that size beside 1 - p.  Sums are fp32 and their order is fixed: the same inputs give the same bits.
+ * dhidden and with dweight.  G is rounded to bf16 before the two products (its relative error, 2^-9 in the mean, is that of
+ * the outputs' own rounding) and counts as 0 below 2^-126 times the largest finite |dloss|.  Its entry at the target comes from
+ * the target's fp32 logit and lse as given: where the target's probability p is near 1, lse's own fp32 rounding (2^-24 |lse|) is
+ * an error of that size beside 1 - p.  Sums are fp32 and their order is fixed: the same inputs give the same bits.
  * hidden, dhidden [rows, D], weight, dweight [V, D]: bf16 with row strides (elements, multiples of 8), 16-byte aligned;
  * target [rows] int32; loss, lse, dloss [rows] fp32.  rows = 0 is allowed (dweight = 0).  D <= TSLT_MAX_HIDDEN, rows <=
  * TSLT_MAX_LOSS_ROWS, V <= TSLT_MAX_VOCAB.  Outputs must not overlap inputs or each other (the same

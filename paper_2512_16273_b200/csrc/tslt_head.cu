@@ -8,12 +8,12 @@
 //
 // Few rows (a decoding step): bound by reading the weight once.  The weight is the operand of the tensor cores' 128 rows and
 // the tokens are its columns (16 ... 160), so that the whole weight goes once through shared memory whatever their number
-// (V = 128256, K = 4096, 32 rows: 87 us, 0.94 of the copy bandwidth).
+// (V = 128256, K = 4096, 32 rows: 90 us on the device, 0.89 of the copy bandwidth).
 //
 // Many rows (verification, prompts): bound by the tensor cores.  The tokens are the rows, 256 of them to a pair of CTAs, and a
 // lane of the epilogue holds 64 consecutive logits of a token, which leave through shared memory as whole 128-byte lines
-// (V = 256000, K = 4096, 2304 rows: 1.77 ms cool, 1.95 ms sustained, 2.5 to 2.7 POPS; cuBLAS's int8 product, which leaves
-// 32-bit sums, 1.54 and 1.93 ms).
+// (V = 256000, K = 4096, 2304 rows: 1.77 ms cool, 1.86 to 1.95 ms sustained, 2.5 to 2.7 POPS; cuBLAS's int8 product, which
+// leaves 32-bit sums, 1.54 and 1.79 to 1.93 ms).
 #include "tslt_gemm.cuh"
 
 namespace tslt {
@@ -233,7 +233,9 @@ template <int kRows, typename T> static int launch_vec(VecParams p, int* status,
 }
 
 // Rows from which the tokens become the tensor cores' rows: few-rows / many-rows form, us, at V = 128256, K = 4096: 128 rows
-// 101 / 110, 160 rows 109 / 112, 192 rows 116 / 115, 256 rows 133 / 117; K = 1024: 128 rows 49 / 52, 192 rows 60 / 57.
+// 101 / 110, 160 rows 109 / 112, 192 rows 116 / 115, 256 rows 133 / 117; K = 1024: 128 rows 49 / 52, 192 rows 60 / 57.  (The few-rows
+// form has one tile of at most 256 columns, so there is nothing to compare behind 256 rows.  The many-rows form computes whole tiles
+// of 256 rows: 257 rows cost what 512 do.)
 constexpr int kManyRows = 161;
 
 template <typename T>

@@ -4,18 +4,25 @@
 // Mathematics.  z = H W^T; lse_n = ln sum_v exp z[n, v]; loss_n = lse_n - z[n, t_n].  With g_n the weight of row n's loss,
 // G[n, v] = g_n (exp(z[n, v] - lse_n) - [v = t_n]), dH = G W, dW = G^T H.
 //
-// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way (backward does the same: where
-// the target's probability is near 1, its entry of G is a small difference, which the tensor cores' truncated sum of z would
-// spoil: off by up to 470 times what lse's own rounding leaves, D = 8192).  One product whose
+// Forward: the rows that count are gathered, and the target's logit is an fp32 dot product on the way.  One product whose
 // epilogue turns each tile of z, still in tensor memory, into (max, sum) pairs, two a row; the pairs of all tiles (16 bytes
 // for 256 logits) go to the workspace and a small kernel joins them.
 // Backward, piece by piece of the vocabulary: z of the piece is computed again and its epilogue writes G of the piece in
 // bf16 to the workspace (as 64-column panels, contiguous whichever of its axes a product reads along); one kernel with two
 // products reads it: the piece's part of dH (summed over the pieces in fp32, in a fixed order) and dW of the piece (complete:
-// its sum runs over the rows).  2 + 6 rows x V x D operations; the recomputation is the price of not keeping rows x V logits.
+// its sum runs over the rows).  The target's entry of G comes from the gather's fp32 dot product again: where its probability is
+// near 1 it is a small difference, which the tensor cores' sum of z would spoil (gradients off by 9 to 470 times what lse's
+// own rounding leaves).  2 + 6 rows x V x D operations: z is computed twice, as rows x V logits are not kept between two calls.
 //
 // Bound by the tensor cores under the power cap (6144 rows, V = 128256, D = 4096, sustained: forward 4.9 ms, a piece of 16128
 // entries z and G 655 us, dH and dW 1250 us; cuBLAS for the three products of a piece alone 627, 612 and 591 us).
+//
+// Rounding.  G is bf16: it is an operand of the tensor cores beside the bf16 weight and hidden rows, and two bf16 parts of it would double
+// the two products that bound the call.  It costs about what the outputs' own rounding does (gradients off by 0.0018 to 0.0019 of
+// their norm, 0.0017 from their rounding alone).  Powers are ex2.approx (2^-22 relative; 0 below 2^-126), a tile's sums
+// of them fp32, their join fp64.  The sums of dH and dW are the tensor cores' fp32: n entries lose n 2^-30 of the sum in the mean
+// (as z does below), 1.5e-5 for a piece of 16128 entries and 5e-4 for the longest (524288, up to 256 rows), below the
+// bf16 outputs' 2^-8; pieces and cuts are added to nearest.
 //
 // Ignored rows (negative target) are taken out before anything is multiplied: the rows that count are copied together, in
 // their order, and every product runs over those only.  Ignored rows cost nothing and what they hold (padding, NaN) is

@@ -5,9 +5,11 @@
 // q = rint(127 y / max|y|) with scale = max|y| / 127.  The row's 1 / rms cancels out of q: q = rint(127 v / max|v|).
 // So the sum of squares and the maximum are needed from ONE pass over the row and one block reduction gives both;
 // the row stays in registers between them and is read and written once: 2 + 2 + 2 + 1 bytes an element (bf16 with a
-// residual).  Bound by HBM once the arithmetic was on pairs: 16384 x 4096 takes 83 us (5.6 TB/s), with values 95 us
-// (6.4 TB/s, 0.97 of the copy bandwidth); element by element it was 113 us at 42 instructions an element, and 102 us with
-// 76 registers a thread instead of 64 (six CTAs of 128 threads on an SM instead of eight).  fp32: 129 us, 6.8 TB/s.
+// residual).  Bound by HBM once the arithmetic was on pairs: 16384 x 4096 takes 80 us (5.8 TB/s), with values 94 us
+// (6.5 TB/s, 0.98 of the copy bandwidth; outputs reused from call to call); element by element it was 113 us at 42
+// instructions an element, and 102 us with 76 registers a thread instead of 64 (six CTAs of 128 threads on an SM instead of
+// eight).  fp32: 126 us, 6.9 TB/s.  The quantiser on a 128256 x 4096 weight: fp32 426 us (6.2 TB/s), bf16 472 us (3.3 TB/s: 0.6 of
+// the bytes, as many instructions).
 //
 // Rounding.  t = v * (127 / max|v|) in fp32 is off by at most 1.5 * 2^-23 * 127 = 2.3e-5; where t lies within 1e-4 of
 // the border between two codes (one element in 5000), the code is taken from the quotient in fp64 instead, so that
@@ -311,7 +313,8 @@ template <typename T, bool kNorm> static int launch_norm(const NormParams& p, cu
     // machine: four vectors in flight per thread where a row has 512 (16384 x 4096, us, 1 / 2 / 4 vectors: bf16 118 / 107 / 95,
     // fp32 329 / 185 / 150).
     const bool many = p.rows >= 2 * 148;
-    if (many && nvec <= 128) {  // a warp holds the row: no barrier, and a quarter of the CTAs to start (16384 x 512 bf16: 18.1 -> 14.8 us)
+    if (many && nvec <= 128) {  // a warp holds the row: no barrier, and a quarter of the CTAs to start (16384 x 512 bf16: 18.1 -> 14.6 us; the
+    // warp's one row leaves nothing in flight during its arithmetic)
         auto kern = nvec > 64 ? norm_quant_kernel<T, 4, kNorm, true> : nvec > 32 ? norm_quant_kernel<T, 2, kNorm, true> : norm_quant_kernel<T, 1, kNorm, true>;
         return gemm::launch_early(kern, dim3((p.rows + 3) / 4), 128, 0, 1, st, p) == cudaSuccess ? TSLT_OK : TSLT_ERR_CUDA;
     }
